@@ -348,6 +348,16 @@ MOE355_API int moe_fp8_fused_forward(const moe_shape *shape, const void *x, cons
                                      const float *topk_w, const moe_dispatch *tables, const void *packed_gate_up,
                                      const void *packed_down, const float *h_scale, void *y, void *workspace,
                                      size_t workspace_bytes, void *stream, void *const *events);
+/*
+ * moe_fp8_fused_forward on token rows that are codes already: codes [T, d] (E4M3, 16-byte aligned) and scales [T] fp32, as
+ * moe_rmsnorm or moe_fp8_quantize_rows writes them; the same workspace and errors, and the same y, bit for bit, for the codes
+ * of moe_fp8_quantize_rows on x.
+ */
+MOE355_API int moe_fp8_fused_forward_codes(const moe_shape *shape, const void *codes, const float *scales,
+                                           const int32_t *topk_idx, const float *topk_w, const moe_dispatch *tables,
+                                           const void *packed_gate_up, const void *packed_down, const float *h_scale,
+                                           void *y, void *workspace, size_t workspace_bytes, void *stream,
+                                           void *const *events);
 
 /*
  * Training path (the paper's end-to-end results cover forward and backward, Sec. V; it gives no formulas: these are
@@ -424,6 +434,98 @@ MOE355_API int moe_fused_backward_bounded(const moe_shape *shape, const void *x,
  */
 MOE355_API int moe_route_backward(const moe_shape *shape, const int32_t *topk_idx, const float *topk_w,
                                   const float *d_topk_w, float *dlogits, void *stream);
+
+/*
+ * Root-mean-square norm in front of the layer, with the addition of the residual and the E4M3 codes of the result for the
+ * FP8 form.  x, residual, sum, y [rows, cols] and weight [cols] in `dtype` (moe_dtype); cols a multiple of 8, at most 32768.
+ *   s = x + residual, rounded to the element type (residual NULL: s = x), written to `sum` if that is not NULL;
+ *   rstd = (mean over the row of s^2 + eps)^(-1/2) in fp32, written to rstd [rows] if that is not NULL;
+ *   y = s rstd weight, formed in fp32 and rounded once, written if y is not NULL;
+ *   codes [rows, cols], scales [rows] (both or neither): scale = largest magnitude of the row's y / 448 (1 for a zero row),
+ *   code = cvt(y / scale), of y before its rounding to the element type.
+ * At least one of y and codes is given; `sum` only with a residual, and it may be x or residual itself; y must be none of the
+ * other arrays.  eps > 0.  Pointers 16-byte aligned (codes 8, scales and rstd 4).  A row with a NaN, an infinity or values whose
+ * squares leave the range of fp32 (magnitudes of about 1e19) has no defined y, and a scale that is not finite where y is not.
+ *
+ * moe_rmsnorm_backward: with a = dy weight,
+ *   dx = rstd (a - s rstd^2 mean(a s)) + dsum,   dweight[c] = sum over the rows of dy s rstd.
+ *   sum: s as the forward wrote it (without a residual: x); rstd as the forward wrote it; dy [rows, cols]; dsum [rows, cols] the
+ *   gradient that reaches s directly, down the residual stream (NULL: none); dx [rows, cols] the gradient of x and of the
+ *   residual alike, it may be dy or dsum itself; dweight [cols] fp32 (NULL: not wanted, and no workspace needed), written in
+ *   full.  Sums in fp32 in an order that depends on the sizes only: same inputs, same bits.  workspace >=
+ *   moe_rmsnorm_backward_workspace_bytes(rows, cols) (0 for invalid sizes), 16-byte aligned; a buffer for more rows serves fewer.
+ */
+MOE355_API int moe_rmsnorm(int64_t rows, int cols, int dtype, const void *x, const void *residual, const void *weight,
+                           float eps, void *sum, void *y, void *codes, float *scales, float *rstd, void *stream);
+MOE355_API size_t moe_rmsnorm_backward_workspace_bytes(int64_t rows, int cols);
+MOE355_API int moe_rmsnorm_backward(int64_t rows, int cols, int dtype, const void *sum, const void *weight,
+                                    const float *rstd, const void *dy, const void *dsum, void *dx, float *dweight,
+                                    void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The experts' rows back to their tokens with the gate weights applied, and the gradients of that and of the sorting copy
+ * (moe_dispatch_gather), for callers that run their own products between the two.  Unlike moe_combine_reduce the rows are
+ * in the element type of the layer and not yet weighted.  rows, d_rows, d_xs [P_cap, d] (layout rows as moe_dispatch_gather
+ * writes them), dy, y, dx [T, d]; pointers 16-byte aligned; topk_idx, topk_w, tables of the batch (perm and the rank arrays are not
+ * read).  Sums in fp32 in slot order, one rounding at the write; what lies behind the last local row is neither read nor written.
+ *
+ * moe_combine_weighted: y[t] = sum over the local slots j of topk_w[t,j] rows[row of (t,j)], zeros where there is none.
+ * moe_combine_weighted_backward: d_rows[row of (t,j)] = topk_w[t,j] dy[t], d_topk_w[t,j] = <rows[row of (t,j)], dy[t]> in fp32
+ *   (0 for a slot whose expert is not local; the array is written in full).  d_rows may be rows itself.
+ * moe_dispatch_gather_backward: dx[t] = sum over the local slots j of d_xs[row of (t,j)], zeros where there is none.
+ */
+MOE355_API int moe_combine_weighted(const moe_shape *shape, const void *rows, const int32_t *topk_idx, const float *topk_w,
+                                    const moe_dispatch *tables, void *y, void *stream);
+MOE355_API int moe_combine_weighted_backward(const moe_shape *shape, const void *rows, const void *dy,
+                                             const int32_t *topk_idx, const float *topk_w, const moe_dispatch *tables,
+                                             void *d_rows, float *d_topk_w, void *stream);
+MOE355_API int moe_dispatch_gather_backward(const moe_shape *shape, const void *d_xs, const int32_t *topk_idx,
+                                            const moe_dispatch *tables, void *dx, void *stream);
+
+/*
+ * One AdamW step over a list of tensors (the weights of a layer, with the gradients of moe_fused_backward), in place:
+ *   g = grad_scale grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps),
+ *   copy = param rounded to bf16 (where copy is not NULL).
+ * The list is read by the host during the call; the arrays are device memory.  param fp32 [n], copy bf16 [n], grad [n] in
+ * grad_dtype, all 16-byte aligned; n = 0 is an empty tensor.  No array may be part of two tensors of one call.
+ *   state_bits 32: m, v fp32 [n], 16-byte aligned; the scales are not read.
+ *   state_bits 8:  m, v uint8 [n], 16-byte aligned, m_scale, v_scale fp32 [ceil(n / MOE_ADAMW_BLOCK)]: E4M3 codes of m / scale and
+ *     of sqrt(v) / scale, one scale per MOE_ADAMW_BLOCK values = largest magnitude / 448 (1 for a block of zeros; a fresh state is
+ *     codes 0).  The step is taken with the new m and v before they are rounded.  A code is rounded up with the probability of the
+ *     part that is cut off, from 16 bits of a hash: with mix(z): z = (z ^ z >> 16) * 0x6A09E667, z = (z ^ z >> 15) * 0xBB67AE85,
+ *     z ^ z >> 16 (mod 2^32), element i of tensor k of the list has h = mix(low word of i ^ mix(high word of i + mix(seed +
+ *     mix(step + mix(k + 0x9E3779B9))))), m its low and sqrt(v) its high half.  A positive sqrt(v) never gets code 0.
+ *     A block that holds a value that is not finite gets the scale NaN.
+ * The step's own numbers, moe_adamw_device: step counts from 1.  They come from config->now, or, where `device` is not NULL, from
+ * that device memory when the kernels run (for captured steps: write it between replays; lr and step are then not checked).
+ * A grad_scale that is not finite leaves every array as it was (a step whose gradients have overflowed is skipped without a
+ * word from the host).  Same inputs, same bits.
+ */
+#define MOE_ADAMW_BLOCK 256
+typedef struct {
+  float lr;
+  float grad_scale;
+  int32_t step;
+  uint32_t seed;
+} moe_adamw_device;
+typedef struct {
+  double beta1, beta2, eps; /* 0 <= beta < 1, eps > 0 */
+  int32_t state_bits;       /* 32 or 8 */
+  moe_adamw_device now;
+} moe_adamw_config;
+typedef struct {
+  float *param;
+  void *copy;
+  const void *grad;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  int64_t n;
+  float weight_decay;
+  int32_t grad_dtype; /* moe_dtype */
+} moe_adamw_tensor;
+MOE355_API int moe_adamw_step(const moe_adamw_config *config, const moe_adamw_tensor *tensors, int count,
+                              const moe_adamw_device *device, void *stream);
 
 /* Static string for a status code. */
 MOE355_API const char *moe_status_string(int status);

@@ -32,6 +32,23 @@ class moe_dispatch(C.Structure):
                                           "dedup_tok", "dedup_mask", "pair_to_dedup")]
 
 
+class moe_adamw_device(C.Structure):
+    _fields_ = [("lr", C.c_float), ("grad_scale", C.c_float), ("step", C.c_int32), ("seed", C.c_uint32)]
+
+
+class moe_adamw_config(C.Structure):
+    _fields_ = [("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("state_bits", C.c_int32),
+                ("now", moe_adamw_device)]
+
+
+class moe_adamw_tensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("param", "copy", "grad", "m", "v", "m_scale", "v_scale")] + \
+        [("n", C.c_int64), ("weight_decay", C.c_float), ("grad_dtype", C.c_int32)]
+
+
+MOE_ADAMW_BLOCK = 256  # values that share a scale in the 8-bit states
+
+
 class MoeError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -113,6 +130,8 @@ def lib() -> C.CDLL:
         L.moe_fp8_quantize_rows.argtypes = [C.c_int64, i32, vp, vp, vp, vp]
         L.moe_fp8_fused_forward.restype = i32
         L.moe_fp8_fused_forward.argtypes = [sp, vp, vp, vp, dp, vp, vp, vp, vp, vp, sz, vp, C.POINTER(vp)]
+        L.moe_fp8_fused_forward_codes.restype = i32
+        L.moe_fp8_fused_forward_codes.argtypes = [sp, vp, vp, vp, vp, dp, vp, vp, vp, vp, vp, sz, vp, C.POINTER(vp)]
         for name in ("moe_train_kept_bytes", "moe_backward_workspace_bytes"):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = [sp]
@@ -131,6 +150,21 @@ def lib() -> C.CDLL:
         L.moe_dispatch_gather.argtypes = [sp, vp, dp, vp, vp]
         L.moe_combine_reduce.restype = i32
         L.moe_combine_reduce.argtypes = [sp, vp, vp, dp, vp, vp]
+        i64 = C.c_int64
+        L.moe_rmsnorm.restype = i32
+        L.moe_rmsnorm.argtypes = [i64, i32, i32, vp, vp, vp, C.c_float, vp, vp, vp, vp, vp, vp]
+        L.moe_rmsnorm_backward_workspace_bytes.restype = sz
+        L.moe_rmsnorm_backward_workspace_bytes.argtypes = [i64, i32]
+        L.moe_rmsnorm_backward.restype = i32
+        L.moe_rmsnorm_backward.argtypes = [i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.moe_combine_weighted.restype = i32
+        L.moe_combine_weighted.argtypes = [sp, vp, vp, vp, dp, vp, vp]
+        L.moe_combine_weighted_backward.restype = i32
+        L.moe_combine_weighted_backward.argtypes = [sp, vp, vp, vp, vp, dp, vp, vp, vp]
+        L.moe_dispatch_gather_backward.restype = i32
+        L.moe_dispatch_gather_backward.argtypes = [sp, vp, vp, dp, vp, vp]
+        L.moe_adamw_step.restype = i32
+        L.moe_adamw_step.argtypes = [C.POINTER(moe_adamw_config), C.POINTER(moe_adamw_tensor), i32, vp, vp]
         L.moe_status_string.restype = C.c_char_p
         L.moe_status_string.argtypes = [i32]
         _lib = L
@@ -410,6 +444,17 @@ def moe_fp8_fused_forward(shape, x, topk_idx, topk_w, tables, packed_gate_up, pa
                                        _ptr(workspace), nbytes, _stream(stream), arr), "moe_fp8_fused_forward")
 
 
+def moe_fp8_fused_forward_codes(shape, codes, scales, topk_idx, topk_w, tables, packed_gate_up, packed_down, h_scale, y,
+                                workspace, events=None, workspace_bytes=None, stream=None) -> None:
+    """moe_fp8_fused_forward on token rows that are codes already, as moe_rmsnorm writes them."""
+    nbytes = workspace.numel() * workspace.element_size() if workspace_bytes is None else workspace_bytes
+    arr = None if events is None else (C.c_void_p * 5)(*[C.c_void_p(int(e)) if e else None for e in events])
+    _check(lib().moe_fp8_fused_forward_codes(C.byref(shape), _ptr(codes), _ptr(scales), _ptr(topk_idx), _ptr(topk_w),
+                                             C.byref(tables.struct), _ptr(packed_gate_up), _ptr(packed_down),
+                                             _ptr(h_scale), _ptr(y), _ptr(workspace), nbytes, _stream(stream), arr),
+           "moe_fp8_fused_forward_codes")
+
+
 def _nbytes(t) -> int:
     return t.numel() * t.element_size()
 
@@ -476,3 +521,41 @@ def moe_dispatch_gather(shape, x, tables, xs, stream=None) -> None:
 def moe_combine_reduce(shape, rows, topk_idx, tables, y, stream=None) -> None:
     _check(lib().moe_combine_reduce(C.byref(shape), _ptr(rows), _ptr(topk_idx), C.byref(tables.struct), _ptr(y),
                                     _stream(stream)), "moe_combine_reduce")
+
+
+def moe_combine_weighted(shape, rows, topk_idx, topk_w, tables, y, stream=None) -> None:
+    _check(lib().moe_combine_weighted(C.byref(shape), _ptr(rows), _ptr(topk_idx), _ptr(topk_w), C.byref(tables.struct),
+                                      _ptr(y), _stream(stream)), "moe_combine_weighted")
+
+
+def moe_combine_weighted_backward(shape, rows, dy, topk_idx, topk_w, tables, d_rows, d_topk_w, stream=None) -> None:
+    _check(lib().moe_combine_weighted_backward(C.byref(shape), _ptr(rows), _ptr(dy), _ptr(topk_idx), _ptr(topk_w),
+                                               C.byref(tables.struct), _ptr(d_rows), _ptr(d_topk_w), _stream(stream)),
+           "moe_combine_weighted_backward")
+
+
+def moe_dispatch_gather_backward(shape, d_xs, topk_idx, tables, dx, stream=None) -> None:
+    _check(lib().moe_dispatch_gather_backward(C.byref(shape), _ptr(d_xs), _ptr(topk_idx), C.byref(tables.struct), _ptr(dx),
+                                              _stream(stream)), "moe_dispatch_gather_backward")
+
+
+def moe_rmsnorm(rows, cols, dtype, x, residual, weight, eps, sum, y, codes, scales, rstd, stream=None) -> None:
+    """`residual`, `sum`, `y`, `codes` with `scales`, and `rstd` may be None as the header says."""
+    _check(lib().moe_rmsnorm(rows, cols, dtype, _ptr(x), _ptr(residual), _ptr(weight), eps, _ptr(sum), _ptr(y), _ptr(codes),
+                             _ptr(scales), _ptr(rstd), _stream(stream)), "moe_rmsnorm")
+
+
+def moe_rmsnorm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().moe_rmsnorm_backward_workspace_bytes(rows, cols))
+
+
+def moe_rmsnorm_backward(rows, cols, dtype, sum, weight, rstd, dy, dsum, dx, dweight, workspace, stream=None) -> None:
+    """`dsum` may be None, and so may `dweight`; `workspace` is then not needed."""
+    _check(lib().moe_rmsnorm_backward(rows, cols, dtype, _ptr(sum), _ptr(weight), _ptr(rstd), _ptr(dy), _ptr(dsum), _ptr(dx),
+                                      _ptr(dweight), _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
+                                      _stream(stream)), "moe_rmsnorm_backward")
+
+
+def moe_adamw_step(config: moe_adamw_config, tensors, count: int, device=None, stream=None) -> None:
+    """`tensors`: a ctypes array of moe_adamw_tensor; `device`: None or the device memory of a moe_adamw_device."""
+    _check(lib().moe_adamw_step(C.byref(config), tensors, count, _ptr(device), _stream(stream)), "moe_adamw_step")

@@ -1,6 +1,6 @@
 // Combine, the phase-split Dispatch copy and the pieces of the unfused comparison path.
 #pragma once
-#include "forward_types.h"
+#include "row_access.h"
 
 namespace moe355 {
 
@@ -11,24 +11,6 @@ namespace moe355 {
 // by its first thread: the same 5.0-5.2 TB/s from HBM, i.e. the rate this machine copies at; loading the rows with
 // the non-temporal hint was 10 % slower.)
 // ------------------------------------------------------------------------------------------------
-// Eight consecutive outputs.  STREAM: with the non-temporal hint (a y row inside the fused call: nothing of the call
-// reads it again, and the next call's operands keep their place in the caches).
-template <typename OutT, bool STREAM = false>
-__device__ __forceinline__ void store8(OutT *dst, const float (&v)[8]) {
-  if constexpr (sizeof(OutT) == 4) {
-    *reinterpret_cast<float4 *>(dst) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4 *>(dst + 4) = make_float4(v[4], v[5], v[6], v[7]);
-  } else {
-    bf16x8 o;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) o[q] = (bf16_t)v[q];
-    if constexpr (STREAM)
-      __builtin_nontemporal_store(o, reinterpret_cast<bf16x8 *>(dst));
-    else
-      *reinterpret_cast<bf16x8 *>(dst) = o;
-  }
-}
-
 // The sum of one token's rows by one wave.  `row` holds, in the lanes named by `slots`, the layout rows of the token's
 // local slots (lane = slot index); the rows are added in slot order, starting from zero, in fp32.  Four pieces of 512
 // columns at a time (8 per lane each) and the loads of two slots in flight together.  poison: write NaN instead.
@@ -87,17 +69,6 @@ __device__ __forceinline__ void combine_token_rows(const float *__restrict__ row
       }
     }
   }
-}
-
-// Layout row of slot `lane` of token t if that slot is local (else -1): one lane per slot.
-__device__ __forceinline__ int combine_slot_row(const int32_t *__restrict__ topk_idx,
-                                                const int32_t *__restrict__ inv_perm, int t, int k, int lane,
-                                                int e_lo, int E_loc, int base, int row_limit) {
-  if (lane >= k) return -1;
-  const int e = topk_idx[(size_t)t * k + lane];
-  if (e < e_lo || e >= e_lo + E_loc) return -1;
-  const int r = inv_perm[(size_t)t * k + lane] - base;
-  return r >= 0 && r < row_limit ? r : -1;
 }
 
 constexpr int kCombineWaves = 4;  // tokens per workgroup of combine_kernel: one per wave

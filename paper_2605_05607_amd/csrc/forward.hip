@@ -459,7 +459,9 @@ static int forward_common(const moe_shape *shape, const void *x, const int32_t *
                           const moe_dispatch *tables, const void *packed_gate_up, const void *packed_down, void *y,
                           void *workspace, size_t workspace_bytes, void *stream, bool fused,
                           void *const *events = nullptr, int gemm_launches = 0, const float *h_scale = nullptr,
-                          void *keep = nullptr, int max_polls = kMaxPolls, int wait_extra = 0) {
+                          void *keep = nullptr, int max_polls = kMaxPolls, int wait_extra = 0,
+                          const float *x_scales = nullptr) {
+  // x_scales != nullptr (FP8 only): x is the tokens' codes already, with these scales
   Derived dv;
   int rc = check_shape(shape, &dv);
   if (rc != MOE_OK) return rc;
@@ -516,7 +518,9 @@ static int forward_common(const moe_shape *shape, const void *x, const int32_t *
     unsigned char *b = static_cast<unsigned char *>(workspace);
     uint8_t *xq = b + L.total;
     float *x_scale = reinterpret_cast<float *>(b + L.total + align_up((size_t)shape->T * shape->d, 256));
-    if (!streams && codes_with_table(shape, dv)) {
+    if (x_scales) {
+      // nothing to quantise
+    } else if (!streams && codes_with_table(shape, dv)) {
       tokens.x = static_cast<const uint4 *>(x);
       tokens.cols = shape->d;
       tokens.codes = xq;
@@ -527,8 +531,8 @@ static int forward_common(const moe_shape *shape, const void *x, const int32_t *
                          static_cast<const uint4 *>(x), shape->d, xq, x_scale);
       if ((rc = launch_status()) != MOE_OK) return rc;
     }
-    q.xq = xq;
-    q.x_scale = x_scale;
+    q.xq = x_scales ? static_cast<const uint8_t *>(x) : xq;
+    q.x_scale = x_scales ? x_scales : x_scale;
     q.gu_scale = reinterpret_cast<const float *>(static_cast<const unsigned char *>(packed_gate_up) +
                                                  align_up(fp8_tile_bytes(shape, dv, 0), 256));
     q.down_scale = reinterpret_cast<const float *>(static_cast<const unsigned char *>(packed_down) +
@@ -657,6 +661,16 @@ extern "C" int moe_fp8_fused_forward(const moe_shape *shape, const void *x, cons
   if (!h_scale) return MOE_ERR_INVALID_ARG;
   return forward_common(shape, x, topk_idx, topk_w, tables, packed_gate_up, packed_down, y, workspace,
                         workspace_bytes, stream, true, events, 0, h_scale);
+}
+
+extern "C" int moe_fp8_fused_forward_codes(const moe_shape *shape, const void *codes, const float *scales,
+                                           const int32_t *topk_idx, const float *topk_w, const moe_dispatch *tables,
+                                           const void *packed_gate_up, const void *packed_down, const float *h_scale,
+                                           void *y, void *workspace, size_t workspace_bytes, void *stream,
+                                           void *const *events) {
+  if (!h_scale || !scales || reinterpret_cast<uintptr_t>(scales) % 4 != 0) return MOE_ERR_INVALID_ARG;
+  return forward_common(shape, codes, topk_idx, topk_w, tables, packed_gate_up, packed_down, y, workspace,
+                        workspace_bytes, stream, true, events, 0, h_scale, nullptr, kMaxPolls, 0, scales);
 }
 
 extern "C" int moe_fused_forward(const moe_shape *shape, const void *x, const int32_t *topk_idx, const float *topk_w,

@@ -1,0 +1,379 @@
+// Root-mean-square norm in front of the layer, with the addition of the residual, the E4M3 codes of the result for the FP8
+// form of the expert GEMMs (reading: one scale per row, largest magnitude / 448) and the gradients.
+//
+//   forward   s = round(x + residual),  rstd = (mean(s^2) + eps)^-1/2,  y = s rstd w
+//   backward  a = dy w,  dx = rstd (a - s rstd^2 mean(a s)) + dsum,  dw = sum over the rows of dy s rstd
+//
+// Bound by HBM: a handful of fp32 operations per element read.  A row stays in the registers of its threads from its one read
+// to its writes; statistics and all sums are fp32, and what is stored in the element type is rounded once.
+#include <algorithm>
+
+#include "forward_types.h"
+
+namespace moe355 {
+
+constexpr int kNormMaxCols = 32768;
+
+// Sixteen bytes of a row.
+template <typename T>
+struct Piece {
+  static constexpr int N = 16 / sizeof(T);
+  uint4 raw;
+  __device__ __forceinline__ void load(const T *p) { raw = *reinterpret_cast<const uint4 *>(p); }
+  __device__ __forceinline__ void zero() { raw = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ float get(int i) const {
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&v)[N]) {
+    if constexpr (sizeof(T) == 4) {
+      return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    } else {
+      bf16x8 o;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) o[q] = (bf16_t)v[q];
+      return __builtin_bit_cast(uint4, o);
+    }
+  }
+};
+
+// Sum or maximum over the WAVES waves of a row; `slot` (LDS) is not used again before the next barrier but one.
+template <int WAVES, typename V, typename OP>
+__device__ __forceinline__ V row_reduce(V v, V *slot, OP op) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v = op(v, __shfl_xor(v, off));
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+    __syncthreads();
+    const int first = (threadIdx.x >> 6) / WAVES * WAVES;
+    v = slot[first];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) v = op(v, slot[first + i]);
+  }
+  return v;
+}
+struct AddF { __device__ float operator()(float a, float b) const { return a + b; } };
+struct MaxU { __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; } };
+
+struct NormArgs {
+  const void *x, *residual, *weight;
+  void *sum, *y;
+  uint8_t *codes;
+  float *scales, *rstd;
+  int64_t rows;
+  int cols;
+  float eps, inv_cols;
+};
+
+// WAVES waves (1: four rows a workgroup, each its own wave; else one row a workgroup) with CHUNKS sixteen-byte pieces a thread.
+template <typename T, int WAVES, int CHUNKS>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_kernel(const NormArgs a) {
+  constexpr int N = Piece<T>::N, STRIDE = WAVES * 64 * N;
+  __shared__ float sums[WAVES == 1 ? 1 : WAVES];
+  __shared__ uint32_t tops[WAVES == 1 ? 1 : WAVES];
+  const int t = WAVES == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
+  const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x;
+  if (row >= a.rows) return;  // (whole waves; with several waves a row never)
+  const int64_t base = row * a.cols;
+  const T *x = static_cast<const T *>(a.x) + base;
+  const T *res = a.residual ? static_cast<const T *>(a.residual) + base : nullptr;
+  const T *wt = static_cast<const T *>(a.weight);
+  Piece<T> v[CHUNKS], w[CHUNKS];
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int c = t * N + i * STRIDE;
+    if (c < a.cols) v[i].load(x + c); else v[i].zero();
+  }
+  if (res) {
+    Piece<T> r[CHUNKS];
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int c = t * N + i * STRIDE;
+      if (c < a.cols) r[i].load(res + c); else r[i].zero();
+    }
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int c = t * N + i * STRIDE;
+      float s[N];
+#pragma unroll
+      for (int q = 0; q < N; ++q) s[q] = v[i].get(q) + r[i].get(q);
+      v[i].raw = Piece<T>::pack(s);  // the norm is that of the stored sum
+      if (a.sum && c < a.cols) *reinterpret_cast<uint4 *>(static_cast<T *>(a.sum) + base + c) = v[i].raw;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int c = t * N + i * STRIDE;
+    if (c < a.cols) w[i].load(wt + c); else w[i].zero();
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+    for (int q = 0; q < N; ++q) ss = fmaf(v[i].get(q), v[i].get(q), ss);
+  ss = row_reduce<WAVES>(ss, sums, AddF());
+  const float rstd = 1.0f / sqrtf(fmaf(ss, a.inv_cols, a.eps));
+  if (a.rstd && t == 0) a.rstd[row] = rstd;
+  if (a.y) {
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int c = t * N + i * STRIDE;
+      float o[N];
+#pragma unroll
+      for (int q = 0; q < N; ++q) o[q] = v[i].get(q) * rstd * w[i].get(q);
+      if (c < a.cols) *reinterpret_cast<uint4 *>(static_cast<T *>(a.y) + base + c) = Piece<T>::pack(o);
+    }
+  }
+  if (!a.codes) return;
+  // Codes of the values before their rounding to the element type.  The maximum is that of the magnitudes' bit patterns, so
+  // that a NaN or an infinity in the row shows as a scale that is not finite.
+  uint32_t top = 0u;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+    for (int q = 0; q < N; ++q) top = MaxU()(top, __float_as_uint(v[i].get(q) * rstd * w[i].get(q)) & 0x7FFFFFFFu);
+  top = row_reduce<WAVES>(top, tops, MaxU());
+  const float amax = __uint_as_float(top);
+  // (2^-120: the reciprocal of a scale below is no normal number)
+  const float scale = top == 0u ? 1.0f : !(amax / 448.0f < 0x1p-120f) ? amax / 448.0f : 0x1p-120f;
+  const float inv = 1.0f / scale;
+  if (t == 0) a.scales[row] = scale;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int c = t * N + i * STRIDE;
+    uint32_t packed[N / 4];
+#pragma unroll
+    for (int g = 0; g < N / 4; ++g) {
+      float q[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        q[j] = __builtin_amdgcn_fmed3f(v[i].get(4 * g + j) * rstd * w[i].get(4 * g + j) * inv, 448.0f, -448.0f);
+      int code = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+      packed[g] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], code, true);
+    }
+    if (c < a.cols) {
+      uint8_t *dst = a.codes + base + c;
+      if constexpr (N == 8)
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(packed[0], packed[1]);
+      else
+        *reinterpret_cast<uint32_t *>(dst) = packed[0];
+    }
+  }
+}
+
+struct NormBackArgs {
+  const void *sum, *weight, *dy, *dsum;
+  const float *rstd;
+  void *dx;
+  float *partial;  // [workgroups][cols] sums of dy s rstd, null without the weight's gradient
+  int64_t rows;
+  int cols;
+  float inv_cols;
+};
+
+// Rows in turn; the threads' columns are the same in every row, so the weight's gradient is summed in registers.  A workgroup
+// has GROUPS rows at a time (each WAVES waves) and writes one partial row.
+template <typename T, int WAVES, int CHUNKS, int GROUPS>
+__global__ __launch_bounds__(WAVES *GROUPS * 64) void rmsnorm_backward_kernel(const NormBackArgs a) {
+  constexpr int N = Piece<T>::N, STRIDE = WAVES * 64 * N;
+  __shared__ float sums[2][WAVES * GROUPS];
+  __shared__ float fold[GROUPS > 1 ? STRIDE : 1];
+  const int group = threadIdx.x / (WAVES * 64), t = threadIdx.x % (WAVES * 64);
+  const T *wt = static_cast<const T *>(a.weight);
+  Piece<T> w[CHUNKS];
+  float dw[CHUNKS][N];
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int c = t * N + i * STRIDE;
+    if (c < a.cols) w[i].load(wt + c); else w[i].zero();
+#pragma unroll
+    for (int q = 0; q < N; ++q) dw[i][q] = 0.f;
+  }
+  int turn = 0;
+  for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < a.rows; first += (int64_t)gridDim.x * GROUPS, turn ^= 1) {
+    const int64_t row = first + group;
+    const bool there = row < a.rows;
+    const int64_t base = row * a.cols;
+    Piece<T> s[CHUNKS], g[CHUNKS];
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int c = t * N + i * STRIDE;
+      if (there && c < a.cols) {
+        s[i].load(static_cast<const T *>(a.sum) + base + c);
+        g[i].load(static_cast<const T *>(a.dy) + base + c);
+      } else {
+        s[i].zero();
+        g[i].zero();
+      }
+    }
+    const float rstd = there ? a.rstd[row] : 0.f;
+    float dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        const float gs = g[i].get(q) * s[i].get(q);
+        dot = fmaf(gs, w[i].get(q), dot);
+        dw[i][q] = fmaf(gs, rstd, dw[i][q]);
+      }
+    dot = row_reduce<WAVES>(dot, sums[turn], AddF());
+    const float mean = dot * a.inv_cols * rstd * rstd;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int c = t * N + i * STRIDE;
+      if (!there || c >= a.cols) continue;
+      Piece<T> r;
+      if (a.dsum) r.load(static_cast<const T *>(a.dsum) + base + c); else r.zero();
+      float o[N];
+#pragma unroll
+      for (int q = 0; q < N; ++q)
+        o[q] = fmaf(rstd, fmaf(-mean, s[i].get(q), g[i].get(q) * w[i].get(q)), r.get(q));
+      *reinterpret_cast<uint4 *>(static_cast<T *>(a.dx) + base + c) = Piece<T>::pack(o);
+    }
+  }
+  if (!a.partial) return;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    if constexpr (GROUPS > 1) {  // the groups' sums in the order of the groups, one piece at a time
+      for (int k = 1; k < GROUPS; ++k) {
+        __syncthreads();
+        if (group == k)
+#pragma unroll
+          for (int q = 0; q < N; ++q) fold[t * N + q] = dw[i][q];
+        __syncthreads();
+        if (group == 0)
+#pragma unroll
+          for (int q = 0; q < N; ++q) dw[i][q] += fold[t * N + q];
+      }
+    }
+    const int c = t * N + i * STRIDE;
+    if (group == 0 && c < a.cols) {
+      float *dst = a.partial + (int64_t)blockIdx.x * a.cols + c;
+#pragma unroll
+      for (int q = 0; q < N; q += 4)
+        *reinterpret_cast<float4 *>(dst + q) = make_float4(dw[i][q], dw[i][q + 1], dw[i][q + 2], dw[i][q + 3]);
+    }
+  }
+}
+
+// dw = the sum of the partial rows in a fixed order: 64 columns a workgroup, its sixteen waves take the rows in turn.
+__global__ __launch_bounds__(1024) void rmsnorm_weight_grad_kernel(const float *__restrict__ partial, int parts, int cols,
+                                                                   float *__restrict__ dw) {
+  __shared__ float part[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  float s = 0.f;
+  if (c < cols)
+#pragma unroll 4
+    for (int p = wave; p < parts; p += 16) s += partial[(int64_t)p * cols + c];
+  part[wave][lane] = s;
+  __syncthreads();
+  if (wave != 0 || c >= cols) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) s += part[i][lane];
+  dw[c] = s;
+}
+
+__global__ void rmsnorm_zero_kernel(float *__restrict__ p, int n) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < n) p[i] = 0.f;
+}
+
+// Waves of a row and pieces of a thread: at most 32 columns a thread, what its registers hold with the sums of the backward pass.
+template <typename T, typename F>
+static void with_row_form(int cols, bool few_rows, F &&f) {
+  const auto at = [&](auto waves) {
+    const int per = ceil_div(cols, decltype(waves)::value * 64 * Piece<T>::N);
+    if (per <= 1) f(waves, std::integral_constant<int, 1>());
+    else if (per <= 2) f(waves, std::integral_constant<int, 2>());
+    else if (per <= 4) f(waves, std::integral_constant<int, 4>());
+    else f(waves, std::integral_constant<int, 32 / Piece<T>::N>());
+  };
+  if (cols <= 2048 && !few_rows) at(std::integral_constant<int, 1>());
+  else if (cols <= 8192 && !few_rows) at(std::integral_constant<int, 4>());
+  else at(std::integral_constant<int, 16>());
+}
+
+constexpr int kNormParts = 1024;  // most partial rows of the weight's gradient
+
+static int norm_check(int64_t rows, int cols, int dtype) {
+  if (rows < 0 || rows > 0x7FFFFFFF || cols < 8 || cols % 8 != 0) return MOE_ERR_INVALID_ARG;
+  if ((dtype != MOE_F32 && dtype != MOE_BF16) || cols > kNormMaxCols) return MOE_ERR_UNSUPPORTED;
+  return MOE_OK;
+}
+
+template <typename T>
+static int norm_forward(const NormArgs &a, hipStream_t st) {
+  with_row_form<T>(a.cols, a.rows < 256, [&](auto waves, auto chunks) {
+    constexpr int W = decltype(waves)::value, C = decltype(chunks)::value;
+    hipLaunchKernelGGL((rmsnorm_kernel<T, W, C>), dim3((unsigned)(W == 1 ? (a.rows + 3) / 4 : a.rows)),
+                       dim3(W == 1 ? 256 : W * 64), 0, st, a);
+  });
+  return launch_status();
+}
+
+template <typename T>
+static int norm_backward(const NormBackArgs &a, float *dweight, hipStream_t st) {
+  int parts = 0;
+  with_row_form<T>(a.cols, false, [&](auto waves, auto chunks) {
+    constexpr int W = decltype(waves)::value, C = decltype(chunks)::value, G = W == 1 ? 4 : 1;
+    parts = (int)std::min<int64_t>(kNormParts, (a.rows + G - 1) / G);
+    hipLaunchKernelGGL((rmsnorm_backward_kernel<T, W, C, G>), dim3((unsigned)parts), dim3(W * G * 64), 0, st, a);
+  });
+  const int rc = launch_status();
+  if (rc != MOE_OK || !dweight) return rc;
+  hipLaunchKernelGGL(rmsnorm_weight_grad_kernel, dim3(ceil_div(a.cols, 64)), dim3(1024), 0, st, a.partial, parts, a.cols,
+                     dweight);
+  return launch_status();
+}
+
+static bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+static bool aligned4(const void *p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
+}  // namespace moe355
+
+using namespace moe355;
+
+extern "C" int moe_rmsnorm(int64_t rows, int cols, int dtype, const void *x, const void *residual, const void *weight,
+                           float eps, void *sum, void *y, void *codes, float *scales, float *rstd, void *stream) {
+  const int rc = norm_check(rows, cols, dtype);
+  if (rc != MOE_OK) return rc;
+  if (!x || !weight || (!y && !codes) || (!codes != !scales) || (sum && !residual)) return MOE_ERR_INVALID_ARG;
+  if (!(eps > 0.f) || !(eps < INFINITY)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(sum) || !aligned16(y) ||
+      reinterpret_cast<uintptr_t>(codes) % 8 != 0 || !aligned4(scales) || !aligned4(rstd))
+    return MOE_ERR_INVALID_ARG;
+  if (y && (y == x || y == residual || y == sum || y == codes)) return MOE_ERR_INVALID_ARG;
+  if (rows == 0) return MOE_OK;
+  NormArgs a{x, residual, weight, sum, y, static_cast<uint8_t *>(codes), scales, rstd, rows, cols, eps, 1.0f / (float)cols};
+  begin_launches();
+  return dtype == MOE_BF16 ? norm_forward<bf16_t>(a, (hipStream_t)stream) : norm_forward<float>(a, (hipStream_t)stream);
+}
+
+extern "C" size_t moe_rmsnorm_backward_workspace_bytes(int64_t rows, int cols) {
+  if (norm_check(rows, cols, MOE_F32) != MOE_OK) return 0;
+  return (size_t)std::max<int64_t>(1, std::min<int64_t>(kNormParts, rows)) * cols * sizeof(float);
+}
+
+extern "C" int moe_rmsnorm_backward(int64_t rows, int cols, int dtype, const void *sum, const void *weight,
+                                    const float *rstd, const void *dy, const void *dsum, void *dx, float *dweight,
+                                    void *workspace, size_t workspace_bytes, void *stream) {
+  int rc = norm_check(rows, cols, dtype);
+  if (rc != MOE_OK) return rc;
+  if (!sum || !weight || !rstd || !dy || !dx) return MOE_ERR_INVALID_ARG;
+  if (dweight && (!workspace || workspace_bytes < moe_rmsnorm_backward_workspace_bytes(rows, cols))) return MOE_ERR_WORKSPACE;
+  if (!aligned16(sum) || !aligned16(weight) || !aligned16(dy) || !aligned16(dsum) || !aligned16(dx) ||
+      !aligned4(rstd) || !aligned4(dweight) || (dweight && !aligned16(workspace)))
+    return MOE_ERR_INVALID_ARG;
+  if (dx == sum) return MOE_ERR_INVALID_ARG;
+  hipStream_t st = (hipStream_t)stream;
+  begin_launches();
+  if (rows == 0) {
+    if (!dweight) return MOE_OK;
+    hipLaunchKernelGGL(rmsnorm_zero_kernel, dim3(ceil_div(cols, 256)), dim3(256), 0, st, dweight, cols);
+    return launch_status();
+  }
+  NormBackArgs a{sum, weight, dy, dsum, rstd, dx, dweight ? static_cast<float *>(workspace) : nullptr, rows, cols,
+                 1.0f / (float)cols};
+  return dtype == MOE_BF16 ? norm_backward<bf16_t>(a, dweight, st) : norm_backward<float>(a, dweight, st);
+}

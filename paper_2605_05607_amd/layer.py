@@ -69,6 +69,38 @@ class MoELayer:
         B.moe_fp8_fused_forward(self.shape, x, self.topk_idx, self.topk_w, self.tables, self.fp8_gate_up,
                                 self.fp8_down, self.h_scale, self.y, self.fp8_ws, events)
 
+    def forward_fp8_codes(self, codes, scales, events=None) -> None:
+        """The FP8 forward on token rows that are codes already (``norm`` writes them)."""
+        B.moe_fp8_fused_forward_codes(self.shape, codes, scales, self.topk_idx, self.topk_w, self.tables, self.fp8_gate_up,
+                                      self.fp8_down, self.h_scale, self.y, self.fp8_ws, events)
+
+    def enable_norm(self, weight, eps: float = 1e-6) -> None:
+        """Buffers of the norm in front of the layer: the sum of the residual stream, the layer's input and its codes."""
+        import torch
+        s, dev = self.shape, self.device
+        self.norm_weight = weight if isinstance(weight, torch.Tensor) else to_device(weight, dev)
+        if self.norm_weight.dtype != self.elt_dtype or self.norm_weight.numel() != s.d:
+            raise ValueError("the norm's weight has d values in the layer's element type")
+        self.norm_eps = eps
+        self.norm_sum, self.x = (torch.empty((max(1, s.T), s.d), dtype=self.elt_dtype, device=dev) for _ in range(2))
+        self.x_codes = torch.empty((max(1, s.T), s.d), dtype=torch.uint8, device=dev)
+        self.x_scales, self.rstd = (torch.empty(max(1, s.T), dtype=torch.float32, device=dev) for _ in range(2))
+        self.norm_ws = torch.empty(max(1, B.moe_rmsnorm_backward_workspace_bytes(s.T, s.d)), dtype=torch.uint8, device=dev)
+        self.d_norm_weight = torch.empty(s.d, dtype=torch.float32, device=dev)
+
+    def norm(self, h, residual=None, codes: bool = False) -> None:
+        """x (and, for forward_fp8_codes, its codes) from the output h of what comes before the layer; with a residual the new
+        one is left in ``norm_sum``."""
+        self._normed = h if residual is None else self.norm_sum
+        B.moe_rmsnorm(self.shape.T, self.shape.d, self.shape.dtype, h, residual, self.norm_weight, self.norm_eps,
+                      None if residual is None else self.norm_sum, self.x, self.x_codes if codes else None,
+                      self.x_scales if codes else None, self.rstd)
+
+    def norm_backward(self, dx, dsum, dh) -> None:
+        """dh from the gradient dx of the layer's input and dsum of the residual stream (or None); d_norm_weight."""
+        B.moe_rmsnorm_backward(self.shape.T, self.shape.d, self.shape.dtype, self._normed, self.norm_weight, self.rstd, dx,
+                               dsum, dh, self.d_norm_weight, self.norm_ws)
+
     def enable_training(self, W_gate: np.ndarray, W_up: np.ndarray, W_down: np.ndarray, wgrad: bool = True) -> None:
         """Buffers of the training path: transposed weight packs, the kept activations, gradients, workspace."""
         import torch
@@ -91,6 +123,20 @@ class MoELayer:
             self.dW_down = torch.empty((El, s.f, s.d), dtype=torch.bfloat16, device=dev)
         else:
             self.dW_gate = self.dW_up = self.dW_down = None
+
+    def enable_optimizer(self, W_gate: np.ndarray, W_up: np.ndarray, W_down: np.ndarray, lr: float, **kw) -> None:
+        """An AdamW step on the three expert weights, after enable_training: fp32 parameters, bf16 copies of them and the
+        optimizer (`kw` as for AdamW)."""
+        import torch
+        self.weights = [to_device(a, self.device) for a in (W_gate, W_up, W_down)]
+        self.masters = [w.to(torch.float32) for w in self.weights]
+        self.optimizer = AdamW(self.masters, [self.dW_gate, self.dW_up, self.dW_down], lr, copies=self.weights, **kw)
+
+    def optimizer_step(self, **kw) -> None:
+        """The step with the gradients of the last `backward`, and the new weights packed for the next forward and backward."""
+        self.optimizer.step(**kw)
+        B.moe_pack_weights(self.shape, *self.weights, self.packed_gate_up, self.packed_down)
+        B.moe_pack_weights_backward(self.shape, *self.weights, self.packed_down_t, self.packed_gate_up_t)
 
     def forward_train(self, x) -> None:
         B.moe_fused_forward_train(self.shape, x, self.topk_idx, self.topk_w, self.tables, self.packed_gate_up,
@@ -143,3 +189,68 @@ class MoELayer:
         """y as float64 on the host (bf16 values widened exactly)."""
         import torch
         return self.y[: self.shape.T].to(torch.float64).cpu().numpy()
+
+
+class AdamW:
+    """One optimizer over a list of fp32 device tensors: holds both states and forwards every step to moe_adamw_step.
+
+    grads: a tensor for each parameter, fp32 or bf16, read by every step.  copies: None, or a bf16 tensor (or None) for each
+    parameter that receives its rounded value.  bits: 32 or 8, the states' width (8: E4M3 codes of m and of sqrt(v), a scale per
+    256 values).  weight_decay: one number, or one for each parameter.  states: [(m, v, m_scale, v_scale)] to go on from, zeros
+    without; steps: steps taken so far.  device_scalars: the step's number, lr and grad_scale live in device memory
+    (``scalars``), so that a captured ``step`` advances with every replay; change them there.
+    """
+
+    def __init__(self, params, grads, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, copies=None, bits=32, seed=0,
+                 states=None, steps=0, device_scalars=False):
+        import torch
+        n = len(params)
+        copies = [None] * n if copies is None else list(copies)
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+        if bits not in (8, 32):
+            raise ValueError("bits is 32 or 8")
+        if not len(grads) == len(copies) == len(decay) == n or (states is not None and len(states) != n):
+            raise ValueError("a gradient, copy, decay and state for each parameter")
+        state = torch.float32 if bits == 32 else torch.uint8
+        if states is None:
+            states = []
+            for p in params:
+                m, v = (torch.zeros(p.numel(), dtype=state, device=p.device) for _ in range(2))
+                scale = (torch.ones(-(-p.numel() // B.MOE_ADAMW_BLOCK), dtype=torch.float32, device=p.device)
+                         for _ in range(2)) if bits == 8 else (None, None)
+                states.append((m, v, *scale))
+        for p, g, c, (m, v, ms, vs) in zip(params, grads, copies, states):
+            blocks = -(-p.numel() // B.MOE_ADAMW_BLOCK)
+            held = [(p, torch.float32, p.numel()), (g, g.dtype, p.numel()), (m, state, p.numel()), (v, state, p.numel())]
+            held += [(c, torch.bfloat16, p.numel())] if c is not None else []
+            held += [(ms, torch.float32, blocks), (vs, torch.float32, blocks)] if bits == 8 else []
+            if g.dtype not in (torch.float32, torch.bfloat16):
+                raise ValueError("gradients are fp32 or bf16")
+            for t, dtype, size in held:
+                if t is None or t.dtype != dtype or t.numel() != size or not t.is_contiguous() or t.device != params[0].device:
+                    raise ValueError("contiguous tensors of the parameter's size on one device: fp32 parameters, bf16 copies")
+        self.params, self.grads, self.copies, self.states = list(params), list(grads), copies, states
+        self.steps = steps
+        self.config = B.moe_adamw_config(beta1, beta2, eps, bits, B.moe_adamw_device(lr, 1.0, 0, seed))
+        self._list = (B.moe_adamw_tensor * max(1, n))(*[
+            B.moe_adamw_tensor(*(B._ptr(t) for t in (p, c, g, *s)), p.numel(), d,
+                               B.MOE_BF16 if g.dtype == torch.bfloat16 else B.MOE_F32)
+            for p, g, c, s, d in zip(params, grads, copies, states, decay)])
+        self.scalars = self._count = None
+        if device_scalars and n:  # a moe_adamw_device: lr and grad_scale as floats, the step's number, the seed
+            words = np.array([lr, 1.0], dtype=np.float32).view(np.int32).tolist() + [steps, int(np.uint32(seed).view(np.int32))]
+            self.scalars = torch.tensor(words, dtype=torch.int32, device=params[0].device)
+            self._count = self.scalars[2:3]
+
+    def step(self, lr=None, grad_scale=1.0) -> None:
+        """One step with the gradients as they are.  lr: a new rate from now on.  With device scalars both are set there."""
+        if self.scalars is not None:
+            if lr is not None or grad_scale != 1.0:
+                raise ValueError("lr and grad_scale are in `scalars`")
+            self._count += 1
+        elif lr is not None:
+            self.config.now.lr = lr
+        self.config.now.grad_scale = grad_scale
+        self.config.now.step = self.steps + 1
+        B.moe_adamw_step(self.config, self._list, len(self.params), self.scalars)
+        self.steps += 1
