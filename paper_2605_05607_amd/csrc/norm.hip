@@ -67,13 +67,14 @@ struct NormArgs {
 };
 
 // WAVES waves (1: four rows a workgroup, each its own wave; else one row a workgroup) with CHUNKS sixteen-byte pieces a thread.
+// 4096 x 7168 in bf16 with residual, sum, y and codes: 46 us, 5.7 TB/s of what it has to move; one row 3.6 us.
 template <typename T, int WAVES, int CHUNKS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_kernel(const NormArgs a) {
   constexpr int N = Piece<T>::N, STRIDE = WAVES * 64 * N;
   __shared__ float sums[WAVES == 1 ? 1 : WAVES];
   __shared__ uint32_t tops[WAVES == 1 ? 1 : WAVES];
   const int t = WAVES == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
-  const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x;
+  const int64_t row = (int64_t)blockIdx.x * (WAVES == 1 ? 4 : 1) + (WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
   if (row >= a.rows) return;  // (whole waves; with several waves a row never)
   const int64_t base = row * a.cols;
   const T *x = static_cast<const T *>(a.x) + base;
@@ -172,14 +173,47 @@ struct NormBackArgs {
   float inv_cols;
 };
 
-// Rows in turn; the threads' columns are the same in every row, so the weight's gradient is summed in registers.  A workgroup
-// has GROUPS rows at a time (each WAVES waves) and writes one partial row.
-template <typename T, int WAVES, int CHUNKS, int GROUPS>
+// What a thread holds of a row.
+template <typename T, int CHUNKS>
+struct NormBackRow {
+  Piece<T> s[CHUNKS], g[CHUNKS], r[CHUNKS];  // s, dy, dsum
+  float rstd;
+  __device__ __forceinline__ void load(const NormBackArgs &a, int64_t row, int t, int stride) {
+    const bool there = row < a.rows;
+    const int64_t base = row * a.cols;
+    rstd = there ? a.rstd[row] : 0.f;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int c = t * Piece<T>::N + i * stride;
+      s[i].zero();
+      g[i].zero();
+      r[i].zero();
+      if (there && c < a.cols) {
+        s[i].load(static_cast<const T *>(a.sum) + base + c);
+        g[i].load(static_cast<const T *>(a.dy) + base + c);
+        if (a.dsum) r[i].load(static_cast<const T *>(a.dsum) + base + c);
+      }
+    }
+  }
+  // Values unpacked before this point are unpacked again behind it: sixteen registers a row less across the barrier.
+  __device__ __forceinline__ void pin() {
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i)
+      asm volatile("" : "+v"(s[i].raw.x), "+v"(s[i].raw.y), "+v"(s[i].raw.z), "+v"(s[i].raw.w), "+v"(g[i].raw.x),
+                   "+v"(g[i].raw.y), "+v"(g[i].raw.z), "+v"(g[i].raw.w));
+  }
+};
+
+// Rows in turn, GROUPS of them at a time (WAVES waves each), the next ones on their way while the sum over a row is formed.  The
+// threads' columns are the same in every row, so the weight's gradient is summed in registers; a workgroup writes one partial row.
+// With the sum over those: 8192 x 4096 in bf16 with dsum 52 us, 5.2 TB/s; 4096 x 7168 47 us, 5.0.
+template <typename T, int WAVES, int CHUNKS, int GROUPS, bool AHEAD>
 __global__ __launch_bounds__(WAVES *GROUPS * 64) void rmsnorm_backward_kernel(const NormBackArgs a) {
   constexpr int N = Piece<T>::N, STRIDE = WAVES * 64 * N;
   __shared__ float sums[2][WAVES * GROUPS];
   __shared__ float fold[GROUPS > 1 ? STRIDE : 1];
-  const int group = threadIdx.x / (WAVES * 64), t = threadIdx.x % (WAVES * 64);
+  // (the same in a wave: rows are addressed from scalar registers)
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (WAVES * 64)), t = threadIdx.x % (WAVES * 64);
   const T *wt = static_cast<const T *>(a.weight);
   Piece<T> w[CHUNKS];
   float dw[CHUNKS][N];
@@ -190,47 +224,36 @@ __global__ __launch_bounds__(WAVES *GROUPS * 64) void rmsnorm_backward_kernel(co
 #pragma unroll
     for (int q = 0; q < N; ++q) dw[i][q] = 0.f;
   }
+  const int64_t step = (int64_t)gridDim.x * GROUPS;
+  int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+  NormBackRow<T, CHUNKS> now, next;
+  now.load(a, row, t, STRIDE);
   int turn = 0;
-  for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < a.rows; first += (int64_t)gridDim.x * GROUPS, turn ^= 1) {
-    const int64_t row = first + group;
-    const bool there = row < a.rows;
-    const int64_t base = row * a.cols;
-    Piece<T> s[CHUNKS], g[CHUNKS];
-#pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
-      const int c = t * N + i * STRIDE;
-      if (there && c < a.cols) {
-        s[i].load(static_cast<const T *>(a.sum) + base + c);
-        g[i].load(static_cast<const T *>(a.dy) + base + c);
-      } else {
-        s[i].zero();
-        g[i].zero();
-      }
-    }
-    const float rstd = there ? a.rstd[row] : 0.f;
+  for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < a.rows; first += step, row += step, turn ^= 1) {
+    if constexpr (AHEAD) next.load(a, row + step, t, STRIDE);
     float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
       for (int q = 0; q < N; ++q) {
-        const float gs = g[i].get(q) * s[i].get(q);
+        const float gs = now.g[i].get(q) * now.s[i].get(q);
         dot = fmaf(gs, w[i].get(q), dot);
-        dw[i][q] = fmaf(gs, rstd, dw[i][q]);
+        dw[i][q] = fmaf(gs, now.rstd, dw[i][q]);
       }
     dot = row_reduce<WAVES>(dot, sums[turn], AddF());
-    const float mean = dot * a.inv_cols * rstd * rstd;
+    if constexpr (AHEAD) now.pin();
+    const float mean = dot * a.inv_cols * now.rstd * now.rstd;
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
       const int c = t * N + i * STRIDE;
-      if (!there || c >= a.cols) continue;
-      Piece<T> r;
-      if (a.dsum) r.load(static_cast<const T *>(a.dsum) + base + c); else r.zero();
+      if (row >= a.rows || c >= a.cols) continue;
       float o[N];
 #pragma unroll
       for (int q = 0; q < N; ++q)
-        o[q] = fmaf(rstd, fmaf(-mean, s[i].get(q), g[i].get(q) * w[i].get(q)), r.get(q));
-      *reinterpret_cast<uint4 *>(static_cast<T *>(a.dx) + base + c) = Piece<T>::pack(o);
+        o[q] = fmaf(now.rstd, fmaf(-mean, now.s[i].get(q), now.g[i].get(q) * w[i].get(q)), now.r[i].get(q));
+      *reinterpret_cast<uint4 *>(static_cast<T *>(a.dx) + row * a.cols + c) = Piece<T>::pack(o);
     }
+    if constexpr (AHEAD) now = next; else now.load(a, row + step, t, STRIDE);
   }
   if (!a.partial) return;
 #pragma unroll
@@ -264,7 +287,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_weight_grad_kernel(const float *
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   float s = 0.f;
   if (c < cols)
-#pragma unroll 4
+#pragma unroll 16
     for (int p = wave; p < parts; p += 16) s += partial[(int64_t)p * cols + c];
   part[wave][lane] = s;
   __syncthreads();
@@ -279,9 +302,11 @@ __global__ void rmsnorm_zero_kernel(float *__restrict__ p, int n) {
   if (i < n) p[i] = 0.f;
 }
 
-// Waves of a row and pieces of a thread: at most 32 columns a thread, what its registers hold with the sums of the backward pass.
+// Waves of a row and pieces of a thread in the forward kernel: at most 32 columns a thread.  Few rows of more than 1024 columns take
+// sixteen waves each, for the latency (64 x 7168: 4.1 us, with eight 4.6; 200 x 2048: 3.9 and with one 4.3; from 256 rows on fewer
+// waves are as fast or faster: 1000 x 2048 6.4 against 8.6).
 template <typename T, typename F>
-static void with_row_form(int cols, bool few_rows, F &&f) {
+static void with_row_form(int64_t rows, int cols, F &&f) {
   const auto at = [&](auto waves) {
     const int per = ceil_div(cols, decltype(waves)::value * 64 * Piece<T>::N);
     if (per <= 1) f(waves, std::integral_constant<int, 1>());
@@ -289,12 +314,18 @@ static void with_row_form(int cols, bool few_rows, F &&f) {
     else if (per <= 4) f(waves, std::integral_constant<int, 4>());
     else f(waves, std::integral_constant<int, 32 / Piece<T>::N>());
   };
-  if (cols <= 2048 && !few_rows) at(std::integral_constant<int, 1>());
-  else if (cols <= 8192 && !few_rows) at(std::integral_constant<int, 4>());
+  const bool few = rows < 256 && cols > 1024;
+  if (cols <= 2048 && !few) at(std::integral_constant<int, 1>());
+  else if (cols <= 4096 && !few) at(std::integral_constant<int, 4>());
+  else if (cols <= 8192 && !few) at(std::integral_constant<int, 8>());
   else at(std::integral_constant<int, 16>());
 }
 
-constexpr int kNormParts = 1024;  // most partial rows of the weight's gradient
+// Workgroups of the backward kernel, each with a partial row of the weight's gradient: one on every CU, eight waves.  With the next
+// rows on their way that fills HBM; more only add partial rows (bf16, us; 4096 x 7168, 8192 x 4096, 16384 x 2048: eight waves and 256
+// workgroups 47.5, 51.8, 51.3, and 512 51.3, 53.9, 53.5; sixteen and 256 56.4, 52.9, 52.8; four and 1024 57.0, 60.3, 56.7).
+constexpr int kNormBackWaves = 8, kNormParts = 256;
+constexpr int64_t kNormLaunchRows = 1 << 21;   // rows of one launch of the forward kernel
 
 static int norm_check(int64_t rows, int cols, int dtype) {
   if (rows < 0 || rows > 0x7FFFFFFF || cols < 8 || cols % 8 != 0) return MOE_ERR_INVALID_ARG;
@@ -303,23 +334,52 @@ static int norm_check(int64_t rows, int cols, int dtype) {
 }
 
 template <typename T>
-static int norm_forward(const NormArgs &a, hipStream_t st) {
-  with_row_form<T>(a.cols, a.rows < 256, [&](auto waves, auto chunks) {
-    constexpr int W = decltype(waves)::value, C = decltype(chunks)::value;
-    hipLaunchKernelGGL((rmsnorm_kernel<T, W, C>), dim3((unsigned)(W == 1 ? (a.rows + 3) / 4 : a.rows)),
-                       dim3(W == 1 ? 256 : W * 64), 0, st, a);
-  });
-  return launch_status();
+static int norm_forward(NormArgs a, hipStream_t st) {
+  const int64_t all = a.rows;
+  for (int64_t first = 0; first < all; first += kNormLaunchRows) {  // (a grid's threads are counted in 32 bits)
+    NormArgs part = a;
+    const int64_t at = first * a.cols;
+    part.x = static_cast<const T *>(a.x) + at;
+    if (a.residual) part.residual = static_cast<const T *>(a.residual) + at;
+    if (a.sum) part.sum = static_cast<T *>(a.sum) + at;
+    if (a.y) part.y = static_cast<T *>(a.y) + at;
+    if (a.codes) part.codes = a.codes + at;
+    if (a.scales) part.scales = a.scales + first;
+    if (a.rstd) part.rstd = a.rstd + first;
+    part.rows = std::min(kNormLaunchRows, all - first);
+    with_row_form<T>(all, a.cols, [&](auto waves, auto chunks) {
+      constexpr int W = decltype(waves)::value, C = decltype(chunks)::value;
+      hipLaunchKernelGGL((rmsnorm_kernel<T, W, C>), dim3((unsigned)(W == 1 ? (part.rows + 3) / 4 : part.rows)),
+                         dim3(W == 1 ? 256 : W * 64), 0, st, part);
+    });
+    const int rc = launch_status();
+    if (rc != MOE_OK) return rc;
+  }
+  return MOE_OK;
 }
 
 template <typename T>
 static int norm_backward(const NormBackArgs &a, float *dweight, hipStream_t st) {
   int parts = 0;
-  with_row_form<T>(a.cols, false, [&](auto waves, auto chunks) {
-    constexpr int W = decltype(waves)::value, C = decltype(chunks)::value, G = W == 1 ? 4 : 1;
+  const auto run = [&](auto waves, auto chunks, auto ahead) {
+    constexpr int W = decltype(waves)::value, G = std::max(1, kNormBackWaves / W), C = decltype(chunks)::value;
     parts = (int)std::min<int64_t>(kNormParts, (a.rows + G - 1) / G);
-    hipLaunchKernelGGL((rmsnorm_backward_kernel<T, W, C, G>), dim3((unsigned)parts), dim3(W * G * 64), 0, st, a);
-  });
+    hipLaunchKernelGGL((rmsnorm_backward_kernel<T, W, C, G, decltype(ahead)::value>), dim3((unsigned)parts), dim3(W * G * 64), 0,
+                       st, a);
+  };
+  const std::integral_constant<int, 1> c1;
+  const std::integral_constant<int, 2> c2;
+  const std::integral_constant<int, 4> c4;
+  const std::integral_constant<int, 8> c8;
+  const std::integral_constant<int, 16> c16;
+  const int waves = ceil_div(a.cols, 64 * 2 * Piece<T>::N);  // with two pieces a thread
+  if (waves <= 1) run(c1, c2, std::true_type());
+  else if (waves <= 2) run(c2, c2, std::true_type());
+  else if (waves <= 4) run(c4, c2, std::true_type());
+  else if (waves <= 8) run(c8, c2, std::true_type());
+  else if (waves <= 16) run(c16, c2, std::true_type());
+  else if (waves <= 32) run(c16, c4, std::false_type());
+  else if constexpr (Piece<T>::N == 4) run(c16, c8, std::false_type());
   const int rc = launch_status();
   if (rc != MOE_OK || !dweight) return rc;
   hipLaunchKernelGGL(rmsnorm_weight_grad_kernel, dim3(ceil_div(a.cols, 64)), dim3(1024), 0, st, a.partial, parts, a.cols,

@@ -105,8 +105,8 @@ def test_forward_and_gradients(rows, cols, dtype):
         # roundings of the three terms; the mean's chain is that of the sum of squares, its error relative to the magnitudes
         size = (r * a).abs() + r ** 3 * s64.abs() * (a * s64).abs().mean(1, keepdim=True)
         assert ((dx.double() - ref_dx).abs() <= size * 2.0 ** -18 + ref_dx.abs() * (half(dt) + 4 * U)).all()
-        # a column's sum: rows / (partial sums) in a register, then at most 1024 partial sums in sixteen chains
-        chain = rows / min(rows, 1024) + 1024 / 16 + 32
+        # a column's sum: rows / (partial sums) in a register, eight registers, then 256 partial sums in sixteen chains
+        chain = rows / min(rows, 256) + 8 + 256 / 16 + 16
         assert ((dw.double() - ref_dw).abs() <= chain * U * (dy.double() * s64 * r).abs().sum(0) + 1e-300).all()
         # without the weight's gradient; into dy or the direct gradient itself; again: the same bits
         for target in (dy.clone(), None if direct is None else direct.clone()):
