@@ -468,6 +468,7 @@ MOE355_API int moe_rmsnorm_backward(int64_t rows, int cols, int dtype, const voi
  * in the element type of the layer and not yet weighted.  rows, d_rows, d_xs [P_cap, d] (layout rows as moe_dispatch_gather
  * writes them), dy, y, dx [T, d]; pointers 16-byte aligned; topk_idx, topk_w, tables of the batch (perm and the rank arrays are not
  * read).  Sums in fp32 in slot order, one rounding at the write; what lies behind the last local row is neither read nor written.
+ * T < 2^24 (MOE_ERR_UNSUPPORTED otherwise).
  *
  * moe_combine_weighted: y[t] = sum over the local slots j of topk_w[t,j] rows[row of (t,j)], zeros where there is none.
  * moe_combine_weighted_backward: d_rows[row of (t,j)] = topk_w[t,j] dy[t], d_topk_w[t,j] = <rows[row of (t,j)], dy[t]> in fp32

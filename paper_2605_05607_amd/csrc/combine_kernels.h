@@ -94,7 +94,8 @@ __global__ __launch_bounds__(kCombineWaves * 64) void combine_kernel(const float
 
 // ------------------------------------------------------------------------------------------------
 // Dispatch as a materialised copy (phase-split entry point): one workgroup per local dedup entry reads the
-// token row once and writes it to the layout row of every slot in the entry's mask.
+// token row once and writes it to the layout row of every slot in the entry's mask, with the non-temporal hint (nothing of
+// the call reads it again; 5003 tokens of 2880: 15 to 11 us, 8192 of 4096: 25 to 24).
 // ------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void dispatch_gather_kernel(const uint4 *__restrict__ x,
                                                               const int32_t *__restrict__ rank_offsets,
@@ -119,7 +120,8 @@ __global__ __launch_bounds__(256) void dispatch_gather_kernel(const uint4 *__res
       m &= m - 1;
       if (j >= k) break;
       const int row = inv_perm[(size_t)t * k + j] - base;
-      if (row >= 0 && row < P_cap) xs[(size_t)row * row_chunks + c] = v;
+      if (row >= 0 && row < P_cap)
+        __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4 *>(xs) + (size_t)row * row_chunks + c);
     }
   }
 }

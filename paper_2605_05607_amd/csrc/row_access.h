@@ -22,22 +22,21 @@ __device__ __forceinline__ void store8(OutT *dst, const float (&v)[8]) {
   }
 }
 
-// Eight columns of a row as floats.
+// Eight columns of a row.
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
+struct Row8 {
+  uint4 raw[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      v[q] = a[q];
-      v[4 + q] = b[q];
-    }
-  } else {
-    const bf16x8 a = *reinterpret_cast<const bf16x8 *>(p);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = (float)a[q];
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = reinterpret_cast<const uint4 *>(p)[i];
   }
-}
+  __device__ __forceinline__ float get(int q) const {
+    const uint4 r = raw[q * (int)sizeof(T) / 16];
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[q & 3]);
+    return __uint_as_float(q & 1 ? w[q >> 1] & 0xFFFF0000u : w[q >> 1] << 16);
+  }
+};
 
 // Layout row of slot `lane` of token t if that slot is local (else -1): one lane per slot.
 __device__ __forceinline__ int combine_slot_row(const int32_t *__restrict__ topk_idx,

@@ -22,9 +22,18 @@ struct RowsArgs {
 };
 
 constexpr int kRowsWaves = 4;  // tokens per workgroup: one per wave
+// Above, a wave takes four pieces of 512 columns and y leaves with the non-temporal hint; up to here one piece, so that there are
+// waves enough, and plain stores.  Microseconds of the two forms (few / many), bf16:
+//   tokens                       64           512          1024         1536          3072
+//   7168, 1 of 8 ranks, k = 8    3.0 / 4.0    5.2 / 5.5    7.1 / 7.3    11.9 / 9.2    22.3 / 18.3
+//   2880, 1 of 4, k = 4          2.8 / 3.4    3.4 / 4.0    4.7 / 4.8     6.0 / 5.6     8.6 / 8.3
+//   2048, 1 of 8, k = 8          2.7 / 3.6    3.1 / 4.0    3.9 / 4.5     4.6 / 5.1     6.8 / 6.9
+//   4096, all local, k = 2       2.8 / 3.3    4.5 / 4.9    6.3 / 6.0     8.6 / 7.7    18.6 / 16.8
+constexpr int kManyTokens = 1024;
 
-// One wave per token and part of its columns (blockIdx.y of gridDim.y parts, taken in turn, 512 columns at a time).
-template <typename T>
+// One wave per token and part of its columns (blockIdx.y of gridDim.y parts, taken in turn): PIECES pieces of 512 columns at a
+// time, and the loads of two slots in flight together.  STREAM: y leaves with the non-temporal hint.
+template <typename T, int PIECES, bool STREAM>
 __global__ __launch_bounds__(kRowsWaves * 64) void combine_rows_kernel(const RowsArgs a) {
   const int lane = threadIdx.x & 63;
   const int t = blockIdx.x * kRowsWaves + (threadIdx.x >> 6);  // wave-uniform
@@ -33,17 +42,46 @@ __global__ __launch_bounds__(kRowsWaves * 64) void combine_rows_kernel(const Row
   const float w = row >= 0 && a.topk_w ? a.topk_w[(size_t)t * a.k + lane] : 1.0f;
   const uint64_t slots = __ballot(row >= 0);
   T *out = static_cast<T *>(a.out) + (size_t)t * a.d;
-  for (int c = lane * 8 + blockIdx.y * 512; c < a.d; c += 512 * gridDim.y) {
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (uint64_t s = slots; s; s &= s - 1) {
-      const int j = __builtin_ctzll(s);
-      const float wj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j));
-      float v[8];
-      load8(static_cast<const T *>(a.rows) + (size_t)__builtin_amdgcn_readlane(row, j) * a.d + c, v);
+  for (int c0 = lane * 8 + blockIdx.y * (512 * PIECES); c0 < a.d; c0 += 512 * PIECES * gridDim.y) {
+    float acc[PIECES][8];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) acc[q] = fmaf(wj, v[q], acc[q]);
+    for (int u = 0; u < PIECES; ++u)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) acc[u][q] = 0.f;
+    for (uint64_t s = slots; s;) {
+      const int j0 = __builtin_ctzll(s);
+      s &= s - 1;
+      const bool two = s != 0;
+      const int j1 = two ? __builtin_ctzll(s) : j0;
+      s &= s - 1;  // (0 stays 0)
+      const T *src0 = static_cast<const T *>(a.rows) + (size_t)__builtin_amdgcn_readlane(row, j0) * a.d;
+      const T *src1 = static_cast<const T *>(a.rows) + (size_t)__builtin_amdgcn_readlane(row, j1) * a.d;
+      Row8<T> v0[PIECES], v1[PIECES];
+#pragma unroll
+      for (int u = 0; u < PIECES; ++u) {
+        const int c = c0 + u * 512;
+        if (c < a.d) {
+          v0[u].load(src0 + c);
+          if (two) v1[u].load(src1 + c);
+        }
+      }
+      const float w0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j0));
+      const float w1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j1));
+#pragma unroll
+      for (int u = 0; u < PIECES; ++u) {
+        if (c0 + u * 512 < a.d) {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) acc[u][q] = fmaf(w0, v0[u].get(q), acc[u][q]);
+          if (two) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) acc[u][q] = fmaf(w1, v1[u].get(q), acc[u][q]);
+          }
+        }
+      }
     }
-    store8<T>(out + c, acc);
+#pragma unroll
+    for (int u = 0; u < PIECES; ++u)
+      if (c0 + u * 512 < a.d) store8<T, STREAM>(out + c0 + u * 512, acc[u]);
   }
 }
 
@@ -66,15 +104,16 @@ __global__ __launch_bounds__(kBackThreads) void combine_rows_backward_kernel(con
     T *dst = static_cast<T *>(a.out) + at;
     float dot = 0.f;
     for (int c = threadIdx.x * 8; c < a.d; c += kBackThreads * 8) {
-      float g[8], v[8], o[8];
-      load8(dy + c, g);
-      load8(src + c, v);
+      Row8<T> g, v;
+      float o[8];
+      g.load(dy + c);
+      v.load(src + c);
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        dot = fmaf(g[q], v[q], dot);
-        o[q] = wj * g[q];
+        dot = fmaf(g.get(q), v.get(q), dot);
+        o[q] = wj * g.get(q);
       }
-      store8<T>(dst + c, o);
+      store8<T, true>(dst + c, o);
     }
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) dot += __shfl_xor(dot, off);
@@ -88,6 +127,7 @@ __global__ __launch_bounds__(kBackThreads) void combine_rows_backward_kernel(con
   a.d_w[(size_t)t * a.k + threadIdx.x] = dot;
 }
 
+constexpr int kMostTokens = 1 << 24;  // a workgroup of 256 threads for each, and a grid's threads are counted in 32 bits
 static bool tables_there(const moe_dispatch *tb) { return tb && tb->offsets && tb->inv_perm; }
 static bool off16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 != 0; }
 
@@ -98,16 +138,18 @@ static int combine_rows(const moe_shape *shape, const void *rows, const int32_t 
   if (rc != MOE_OK) return rc;
   if (!rows || !topk_idx || !tables_there(tables) || !out) return MOE_ERR_INVALID_ARG;
   if (off16(rows) || off16(out) || rows == out) return MOE_ERR_INVALID_ARG;
+  if (shape->T >= kMostTokens) return MOE_ERR_UNSUPPORTED;
   if (shape->T == 0) return MOE_OK;
   RowsArgs a{rows, nullptr, topk_idx, tables->inv_perm, tables->offsets, topk_w, out, nullptr,
              shape->T, shape->k, shape->d, dv.e_lo, dv.E_loc, (int)dv.P_cap};
-  const int parts = std::max(1, std::min(ceil_div(shape->d, 512), 4096 / shape->T));
-  const dim3 grid((unsigned)ceil_div(shape->T, kRowsWaves), (unsigned)parts);
+  const bool many = shape->T > kManyTokens;
+  const dim3 grid((unsigned)ceil_div(shape->T, kRowsWaves), (unsigned)std::min(65535, ceil_div(shape->d, many ? 2048 : 512)));
+  const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kRowsWaves * 64), 0, (hipStream_t)stream, a); };
   begin_launches();
   if (shape->dtype == MOE_BF16)
-    hipLaunchKernelGGL(combine_rows_kernel<bf16_t>, grid, dim3(kRowsWaves * 64), 0, (hipStream_t)stream, a);
+    many ? launch(combine_rows_kernel<bf16_t, 4, true>) : launch(combine_rows_kernel<bf16_t, 1, false>);
   else
-    hipLaunchKernelGGL(combine_rows_kernel<float>, grid, dim3(kRowsWaves * 64), 0, (hipStream_t)stream, a);
+    many ? launch(combine_rows_kernel<float, 4, true>) : launch(combine_rows_kernel<float, 1, false>);
   return launch_status();
 }
 
@@ -134,15 +176,14 @@ extern "C" int moe_combine_weighted_backward(const moe_shape *shape, const void 
   if (rc != MOE_OK) return rc;
   if (!rows || !dy || !topk_idx || !topk_w || !tables_there(tables) || !d_rows || !d_topk_w) return MOE_ERR_INVALID_ARG;
   if (off16(rows) || off16(dy) || off16(d_rows) || d_rows == dy) return MOE_ERR_INVALID_ARG;
+  if (shape->T >= kMostTokens) return MOE_ERR_UNSUPPORTED;
   if (shape->T == 0) return MOE_OK;
   RowsArgs a{rows, dy, topk_idx, tables->inv_perm, tables->offsets, topk_w, d_rows, d_topk_w,
              shape->T, shape->k, shape->d, dv.e_lo, dv.E_loc, (int)dv.P_cap};
+  const auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)shape->T), dim3(kBackThreads), 0, (hipStream_t)stream, a);
+  };
   begin_launches();
-  if (shape->dtype == MOE_BF16)
-    hipLaunchKernelGGL(combine_rows_backward_kernel<bf16_t>, dim3((unsigned)shape->T), dim3(kBackThreads), 0,
-                       (hipStream_t)stream, a);
-  else
-    hipLaunchKernelGGL(combine_rows_backward_kernel<float>, dim3((unsigned)shape->T), dim3(kBackThreads), 0,
-                       (hipStream_t)stream, a);
+  shape->dtype == MOE_BF16 ? launch(combine_rows_backward_kernel<bf16_t>) : launch(combine_rows_backward_kernel<float>);
   return launch_status();
 }
