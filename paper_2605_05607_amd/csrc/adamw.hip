@@ -19,8 +19,9 @@ namespace moe355 {
 
 constexpr int kAdamBlock = MOE_ADAMW_BLOCK;
 constexpr int kAdamThreads = 256;
-constexpr int kAdamChunk = 4096;  // values of one workgroup
 constexpr int kAdamTensors = 40;  // of one launch: their descriptions travel as kernel arguments
+constexpr int64_t kAdamGroups = (1 << 24) - 1;        // workgroups of one launch (their threads are counted in 32 bits)
+constexpr int64_t kAdamMost = kAdamGroups * 2048;     // values of a tensor: 3.4e10
 
 struct AdamTensor {
   float *param;
@@ -54,34 +55,17 @@ struct AdamStep {
   float beta1, beta2, new1, new2, eps, keep, rate, root2, grad_scale;
 };
 
-template <bool BF16>
-__device__ __forceinline__ void load_grad(const void *grad, int64_t i, float (&g)[4]) {
-  if constexpr (BF16) {
-    const uint2 raw = *reinterpret_cast<const uint2 *>(static_cast<const bf16_t *>(grad) + i);
-    g[0] = __uint_as_float(raw.x << 16);
-    g[1] = __uint_as_float(raw.x & 0xFFFF0000u);
-    g[2] = __uint_as_float(raw.y << 16);
-    g[3] = __uint_as_float(raw.y & 0xFFFF0000u);
-  } else {
-    const f32x4 raw = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(grad) + i);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) g[q] = raw[q];
-  }
-}
-__device__ __forceinline__ float grad_at(const void *grad, bool bf16, int64_t i) {
-  return bf16 ? (float)static_cast<const bf16_t *>(grad)[i] : static_cast<const float *>(grad)[i];
-}
-
 // New m, v, sqrt(v) and parameter of one element.  The states' operations round one by one (no contraction, the correctly
 // rounded square root): where a state is held in codes, the last bit of a value can decide which code it gets, and this way the
 // codes are those of the formulas evaluated in fp32 by anyone.
+template <bool EIGHT>
 __device__ __forceinline__ void adam_element(const AdamStep &s, float g, float &p, float &m, float &v, float &root) {
   {
 #pragma clang fp contract(off)
     g = g * s.grad_scale;
     m = s.beta1 * m + s.new1 * g;
     v = s.beta2 * v + s.new2 * g * g;
-    root = sqrtf(v);
+    root = EIGHT ? sqrtf(v) : __builtin_amdgcn_sqrtf(v);
   }
   p = fmaf(p, s.keep, -s.rate * m * __builtin_amdgcn_rcpf(fmaf(root, s.root2, s.eps)));
 }
@@ -97,19 +81,32 @@ __device__ __forceinline__ uint32_t e4m3_stochastic(float v, float scale, float 
   return (up >> 20) - (small ? 968u : 960u);
 }
 
+// The largest of a wave's values: neighbours, quarters and halves of a row of 16 lanes, then rows, by moves between lanes.
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ uint32_t max_of_lanes(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false));  // (0 where nothing comes in)
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max_of_lanes<0xB1>(v);          // quad_perm 1 0 3 2
+  v = max_of_lanes<0x4E>(v);          // quad_perm 2 3 0 1
+  v = max_of_lanes<0x124>(v);         // row_ror 4
+  v = max_of_lanes<0x128>(v);         // row_ror 8
+  v = max_of_lanes<0x142, 0xA>(v);    // lane 15 of a row to the next (rows 1 and 3)
+  v = max_of_lanes<0x143, 0xC>(v);    // lane 31 to rows 2 and 3
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
 struct BlockScale {
   float scale, inv;
 };
 // The scale of the 256 values of a wave, from the largest bit pattern of their magnitudes (a NaN or an infinity gives a scale
 // of NaN, so that the block shows it).  Below 2^-100 a block counts as zero: the reciprocal of its scale is no normal number.
 __device__ __forceinline__ BlockScale block_scale(uint32_t top) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
-  const float amax = __uint_as_float(top);
-  if (top >= 0x7F800000u) return {__builtin_nanf(""), 0.0f};
-  if (amax < 0x1p-100f) return {1.0f, amax == 0.0f ? 1.0f : 0.0f};
-  const float scale = amax * (1.0f / 448.0f);
-  return {scale, 1.0f / scale};
+  top = wave_max(top);
+  const bool finite = top < 0x7F800000u, some = top >= 0x0D800000u;
+  const float scale = some ? __uint_as_float(top) * (1.0f / 448.0f) : 1.0f;
+  const float r = __builtin_amdgcn_rcpf(scale);
+  return {finite ? scale : __builtin_nanf(""), finite && some ? fmaf(fmaf(-scale, r, 1.0f), r, r) : 0.0f};
 }
 
 __device__ __forceinline__ float decode(uint32_t codes, int q) {
@@ -121,13 +118,184 @@ __device__ __forceinline__ float decode(uint32_t codes, int q) {
   }
 }
 
-// A workgroup takes 4096 values of a tensor, a wave 256 at a time, a lane four that lie side by side.
-template <bool EIGHT>
+// Four values that lie side by side, as they are read: the gradient in fp32 or (words 0 and 1) bf16, the states in fp32 or (word
+// 0) codes with their block's scales.
+template <bool EIGHT, bool BF16>
+struct AdamQuad {
+  f32x4 p;
+  u32x4 g, m, v;
+  float m_scale, v_scale;
+
+  __device__ __forceinline__ void load(const AdamTensor &x, int64_t i, int64_t block) {
+    p = *reinterpret_cast<const f32x4 *>(x.param + i);
+    if constexpr (BF16) {
+      const uint2 r = *reinterpret_cast<const uint2 *>(static_cast<const bf16_t *>(x.grad) + i);
+      g[0] = r.x;
+      g[1] = r.y;
+    } else {
+      g = *reinterpret_cast<const u32x4 *>(static_cast<const float *>(x.grad) + i);
+    }
+    if constexpr (EIGHT) {
+      m[0] = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(x.m) + i);
+      v[0] = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(x.v) + i);
+      m_scale = x.m_scale[block];
+      v_scale = x.v_scale[block];
+    } else {
+      m = *reinterpret_cast<const u32x4 *>(static_cast<const float *>(x.m) + i);
+      v = *reinterpret_cast<const u32x4 *>(static_cast<const float *>(x.v) + i);
+    }
+  }
+  // the first `here` of the four (a tensor's end), zeros behind them
+  __device__ __forceinline__ void load(const AdamTensor &x, int64_t i, int64_t block, int here) {
+    p = f32x4{0.f, 0.f, 0.f, 0.f};
+    g = m = v = u32x4{0u, 0u, 0u, 0u};
+    m_scale = v_scale = 0.f;
+    if (EIGHT) {
+      m_scale = x.m_scale[block];
+      v_scale = x.v_scale[block];
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      if (q >= here) continue;
+      p[q] = x.param[i + q];
+      if constexpr (BF16)
+        g[q >> 1] |= (uint32_t)static_cast<const uint16_t *>(x.grad)[i + q] << (16 * (q & 1));
+      else
+        g[q] = static_cast<const uint32_t *>(x.grad)[i + q];
+      if constexpr (EIGHT) {
+        m[0] |= (uint32_t)static_cast<const uint8_t *>(x.m)[i + q] << (8 * q);
+        v[0] |= (uint32_t)static_cast<const uint8_t *>(x.v)[i + q] << (8 * q);
+      } else {
+        m[q] = static_cast<const uint32_t *>(x.m)[i + q];
+        v[q] = static_cast<const uint32_t *>(x.v)[i + q];
+      }
+    }
+  }
+  __device__ __forceinline__ float grad(int q) const {
+    if constexpr (BF16) return __uint_as_float(q & 1 ? g[q >> 1] & 0xFFFF0000u : g[q >> 1] << 16);
+    return __uint_as_float(g[q]);
+  }
+
+  // The step, in place: p, and m and v as they are stored (EIGHT: codes; the new scales go to memory).
+  __device__ __forceinline__ void step(const AdamStep &s, const AdamTensor &x, int64_t i, int64_t block, uint32_t key) {
+    float fm[4], fv[4], root[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (EIGHT) {
+        fm[q] = decode(m[0], q) * m_scale;
+        const float r = decode(v[0], q) * v_scale;
+        fv[q] = r * r;
+      } else {
+        fm[q] = __uint_as_float(m[q]);
+        fv[q] = __uint_as_float(v[q]);
+      }
+      float fp = p[q];
+      adam_element<EIGHT>(s, grad(q), fp, fm[q], fv[q], root[q]);
+      p[q] = fp;
+    }
+    if constexpr (!EIGHT) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        m[q] = __float_as_uint(fm[q]);
+        v[q] = __float_as_uint(fv[q]);
+      }
+    } else {
+      uint32_t top_m = 0u, top_v = 0u;  // (zeros behind the tensor's end)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        top_m = max(top_m, __float_as_uint(fm[q]) & 0x7FFFFFFFu);
+        top_v = max(top_v, __float_as_uint(root[q]) & 0x7FFFFFFFu);
+      }
+      const BlockScale bm = block_scale(top_m), bv = block_scale(top_v);
+      if ((threadIdx.x & 63) == 0) {
+        x.m_scale[block] = bm.scale;
+        x.v_scale[block] = bv.scale;
+      }
+      const uint32_t high = mix(key + (uint32_t)(i >> 32));
+      m[0] = v[0] = 0u;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t h = mix(((uint32_t)i + q) ^ high);
+        const uint32_t cm = e4m3_stochastic(fm[q], bm.scale, bm.inv, h & 0xFFFFu) | (__float_as_uint(fm[q]) >> 31 << 7);
+        const uint32_t cv = e4m3_stochastic(root[q], bv.scale, bv.inv, h >> 16);
+        m[0] |= cm << (8 * q);
+        v[0] |= (root[q] > 0.f ? max(cv, 1u) : cv) << (8 * q);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void store(const AdamTensor &x, int64_t i) const {
+    *reinterpret_cast<f32x4 *>(x.param + i) = p;
+    if (x.copy) *reinterpret_cast<bf16x4 *>(x.copy + i) = bf16x4{(bf16_t)p[0], (bf16_t)p[1], (bf16_t)p[2], (bf16_t)p[3]};
+    if constexpr (EIGHT) {
+      *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(x.m) + i) = m[0];
+      *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(x.v) + i) = v[0];
+    } else {
+      *reinterpret_cast<u32x4 *>(static_cast<float *>(x.m) + i) = m;
+      *reinterpret_cast<u32x4 *>(static_cast<float *>(x.v) + i) = v;
+    }
+  }
+  __device__ __forceinline__ void store(const AdamTensor &x, int64_t i, int here) const {
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      if (q >= here) continue;
+      x.param[i + q] = p[q];
+      if (x.copy) x.copy[i + q] = (bf16_t)p[q];
+      if constexpr (EIGHT) {
+        static_cast<uint8_t *>(x.m)[i + q] = (uint8_t)(m[0] >> (8 * q));
+        static_cast<uint8_t *>(x.v)[i + q] = (uint8_t)(v[0] >> (8 * q));
+      } else {
+        static_cast<uint32_t *>(x.m)[i + q] = m[q];
+        static_cast<uint32_t *>(x.v)[i + q] = v[q];
+      }
+    }
+  }
+};
+
+// PER blocks of 256 values for a wave, a workgroup's waves side by side.  Whole chunks are read before the first block is worked on.
+// 32-bit states: two.  8-bit states, whose blocks take 300 vector instructions each: four where a launch has the values to fill the
+// chip with that, else one (bf16 gradients and copies, 2^17 / 2^19 / 2^21 / 2^23 / 2^25 values: one block 4.4, 5.3, 12.6, 34.0 and
+// 115.8 us, two 5.1, 5.5, 12.9, 32.6 and 108.2, four 6.8, 7.3, 14.1, 32.9 and 105.4).
+constexpr int kAdamFew = 1 << 21;
+constexpr int64_t adam_chunk_values(int per) { return (int64_t)per * kAdamThreads * 4; }
+template <bool EIGHT, bool BF16, int PER>
+__device__ __forceinline__ void adam_chunk(const AdamTensor &x, const AdamStep &s, int64_t begin, uint32_t key) {
+  constexpr int64_t CHUNK = adam_chunk_values(PER);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t first = begin + wave * kAdamBlock;
+  AdamQuad<EIGHT, BF16> quad[PER];
+  if (begin + CHUNK <= x.n) {
+#pragma unroll
+    for (int b = 0; b < PER; ++b) {
+      const int64_t at = first + b * (kAdamThreads * 4);
+      quad[b].load(x, at + lane * 4, at / kAdamBlock);
+    }
+#pragma unroll
+    for (int b = 0; b < PER; ++b) {
+      const int64_t at = first + b * (kAdamThreads * 4);
+      quad[b].step(s, x, at + lane * 4, at / kAdamBlock, key);
+      quad[b].store(x, at + lane * 4);
+    }
+    return;
+  }
+  for (int64_t at = first; at < min(x.n, begin + CHUNK); at += kAdamThreads * 4) {  // (the same in a wave)
+    const int64_t i = at + lane * 4;
+    const int here = (int)max((int64_t)0, min((int64_t)4, x.n - i));
+    AdamQuad<EIGHT, BF16> one;
+    if (here == 4) one.load(x, i, at / kAdamBlock); else one.load(x, i, at / kAdamBlock, here);
+    one.step(s, x, i, at / kAdamBlock, key);
+    if (here == 4) one.store(x, i); else one.store(x, i, here);
+  }
+}
+
+template <bool EIGHT, int PER>
 __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
   const moe_adamw_device now = a.device ? *a.device : a.now;
   if (!(fabsf(now.grad_scale) < INFINITY)) return;  // nothing is changed
-  int k = 0;
-  while (k + 1 < a.count && blockIdx.x >= a.first[k + 1]) ++k;
+  // the tensor of this workgroup: a lane for each
+  const int lane = threadIdx.x & 63;
+  const int k = __builtin_amdgcn_readfirstlane(
+      (int)__popcll(__ballot(lane + 1 < a.count && blockIdx.x >= a.first[min(lane + 1, kAdamTensors)])));
   const AdamTensor &x = a.tensor[k];
   AdamStep s;
   s.beta1 = a.beta1;
@@ -139,111 +307,9 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
   s.rate = now.lr / -expm1f((float)now.step * a.log_beta1);  // (1 - b^t without the cancellation)
   s.root2 = 1.0f / sqrtf(-expm1f((float)now.step * a.log_beta2));
   s.grad_scale = now.grad_scale;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t begin = (int64_t)(blockIdx.x - a.first[k]) * kAdamChunk;
+  const int64_t begin = (int64_t)(blockIdx.x - a.first[k]) * adam_chunk_values(PER);
   const uint32_t key = EIGHT ? mix(now.seed + mix((uint32_t)now.step + mix((uint32_t)(a.index0 + k) + 0x9E3779B9u))) : 0u;
-#pragma unroll
-  for (int b = 0; b < kAdamChunk / (kAdamThreads * 4); ++b) {
-    const int64_t first = begin + (b * (kAdamThreads / 64) + wave) * kAdamBlock;
-    if (first >= x.n) break;  // (the same in a wave)
-    const int64_t i = first + lane * 4;
-    const int here = (int)max((int64_t)0, min((int64_t)4, x.n - i));
-    float p[4], g[4], m[4], v[4], root[4];
-    const int64_t block = first / kAdamBlock;
-    if (here == 4) {
-      if (x.grad_bf16) load_grad<true>(x.grad, i, g); else load_grad<false>(x.grad, i, g);
-      const f32x4 pv = *reinterpret_cast<const f32x4 *>(x.param + i);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) p[q] = pv[q];
-      if constexpr (EIGHT) {
-        const uint32_t mc = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(x.m) + i);
-        const uint32_t vc = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(x.v) + i);
-        const float ms = x.m_scale[block], vs = x.v_scale[block];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          m[q] = decode(mc, q) * ms;
-          const float r = decode(vc, q) * vs;
-          v[q] = r * r;
-        }
-      } else {
-        const f32x4 mv = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(x.m) + i);
-        const f32x4 vv = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(x.v) + i);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          m[q] = mv[q];
-          v[q] = vv[q];
-        }
-      }
-    } else {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        p[q] = g[q] = m[q] = v[q] = 0.f;
-        if (q >= here) continue;
-        g[q] = grad_at(x.grad, x.grad_bf16, i + q);
-        p[q] = x.param[i + q];
-        if constexpr (EIGHT) {
-          m[q] = decode(static_cast<const uint8_t *>(x.m)[i + q], 0) * x.m_scale[block];
-          const float r = decode(static_cast<const uint8_t *>(x.v)[i + q], 0) * x.v_scale[block];
-          v[q] = r * r;
-        } else {
-          m[q] = static_cast<const float *>(x.m)[i + q];
-          v[q] = static_cast<const float *>(x.v)[i + q];
-        }
-      }
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) adam_element(s, g[q], p[q], m[q], v[q], root[q]);
-    uint32_t mc = 0u, vc = 0u;
-    if constexpr (EIGHT) {
-      uint32_t top_m = 0u, top_v = 0u;
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (q < here) {
-          top_m = max(top_m, __float_as_uint(m[q]) & 0x7FFFFFFFu);
-          top_v = max(top_v, __float_as_uint(root[q]) & 0x7FFFFFFFu);
-        }
-      const BlockScale bm = block_scale(top_m), bv = block_scale(top_v);
-      if (lane == 0) {
-        x.m_scale[block] = bm.scale;
-        x.v_scale[block] = bv.scale;
-      }
-      const uint32_t high = mix(key + (uint32_t)(i >> 32));
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint32_t h = mix(((uint32_t)i + q) ^ high);
-        const uint32_t cm = e4m3_stochastic(m[q], bm.scale, bm.inv, h & 0xFFFFu) | (__float_as_uint(m[q]) >> 31 << 7);
-        uint32_t cv = e4m3_stochastic(root[q], bv.scale, bv.inv, h >> 16);
-        cv = root[q] > 0.f ? max(cv, 1u) : cv;
-        mc |= cm << (8 * q);
-        vc |= cv << (8 * q);
-      }
-    }
-    if (here == 4) {
-      *reinterpret_cast<f32x4 *>(x.param + i) = f32x4{p[0], p[1], p[2], p[3]};
-      if (x.copy) *reinterpret_cast<bf16x4 *>(x.copy + i) = bf16x4{(bf16_t)p[0], (bf16_t)p[1], (bf16_t)p[2], (bf16_t)p[3]};
-      if constexpr (EIGHT) {
-        *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(x.m) + i) = mc;
-        *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(x.v) + i) = vc;
-      } else {
-        *reinterpret_cast<f32x4 *>(static_cast<float *>(x.m) + i) = f32x4{m[0], m[1], m[2], m[3]};
-        *reinterpret_cast<f32x4 *>(static_cast<float *>(x.v) + i) = f32x4{v[0], v[1], v[2], v[3]};
-      }
-    } else {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (q >= here) continue;
-        x.param[i + q] = p[q];
-        if (x.copy) x.copy[i + q] = (bf16_t)p[q];
-        if constexpr (EIGHT) {
-          static_cast<uint8_t *>(x.m)[i + q] = (uint8_t)(mc >> (8 * q));
-          static_cast<uint8_t *>(x.v)[i + q] = (uint8_t)(vc >> (8 * q));
-        } else {
-          static_cast<float *>(x.m)[i + q] = m[q];
-          static_cast<float *>(x.v)[i + q] = v[q];
-        }
-      }
-    }
-  }
+  if (x.grad_bf16) adam_chunk<EIGHT, true, PER>(x, s, begin, key); else adam_chunk<EIGHT, false, PER>(x, s, begin, key);
 }
 
 }  // namespace moe355
@@ -264,7 +330,7 @@ extern "C" int moe_adamw_step(const moe_adamw_config *config, const moe_adamw_te
     const moe_adamw_tensor &t = tensors[k];
     if (t.n < 0 || !(t.weight_decay >= 0.f && t.weight_decay < INFINITY)) return MOE_ERR_INVALID_ARG;
     if (t.grad_dtype != MOE_F32 && t.grad_dtype != MOE_BF16) return MOE_ERR_UNSUPPORTED;
-    if (t.n > (int64_t)kAdamChunk << 30) return MOE_ERR_UNSUPPORTED;
+    if (t.n > kAdamMost) return MOE_ERR_UNSUPPORTED;
     if (t.n == 0) continue;
     if (!t.param || !t.grad || !t.m || !t.v || (eight && (!t.m_scale || !t.v_scale))) return MOE_ERR_INVALID_ARG;
     const auto at = [](const void *p) { return reinterpret_cast<uintptr_t>(p); };
@@ -275,11 +341,14 @@ extern "C" int moe_adamw_step(const moe_adamw_config *config, const moe_adamw_te
   for (int k = 0; k < count;) {
     AdamArgs a{};
     a.index0 = k;
+    int64_t values = 0;
+    for (int i = k; i < std::min(count, k + kAdamTensors) && values <= kAdamFew; ++i) values += tensors[i].n;
+    const int per = !eight ? 2 : values > kAdamFew ? 4 : 1;
     int64_t groups = 0;
     for (; k < count && a.count < kAdamTensors; ++k) {
       const moe_adamw_tensor &t = tensors[k];
-      const int64_t more = (t.n + kAdamChunk - 1) / kAdamChunk;
-      if (groups + more > (int64_t)1 << 30) break;  // (the next launch: a tensor alone has at most that many)
+      const int64_t more = (t.n + adam_chunk_values(per) - 1) / adam_chunk_values(per);
+      if (groups + more > kAdamGroups) break;  // (the next launch: a tensor alone has at most that many)
       AdamTensor &x = a.tensor[a.count];
       x.param = t.param;
       x.copy = static_cast<bf16_t *>(t.copy);
@@ -305,10 +374,10 @@ extern "C" int moe_adamw_step(const moe_adamw_config *config, const moe_adamw_te
     a.log_beta2 = (float)std::log(c.beta2);
     a.now = c.now;
     a.device = device;
-    if (eight)
-      hipLaunchKernelGGL(adamw_kernel<true>, dim3((unsigned)groups), dim3(kAdamThreads), 0, (hipStream_t)stream, a);
-    else
-      hipLaunchKernelGGL(adamw_kernel<false>, dim3((unsigned)groups), dim3(kAdamThreads), 0, (hipStream_t)stream, a);
+    const auto launch = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kAdamThreads), 0, (hipStream_t)stream, a);
+    };
+    !eight ? launch(adamw_kernel<false, 2>) : per == 4 ? launch(adamw_kernel<true, 4>) : launch(adamw_kernel<true, 1>);
     const int rc = launch_status();
     if (rc != MOE_OK) return rc;
   }

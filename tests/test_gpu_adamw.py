@@ -254,7 +254,7 @@ def test_values_between_the_tensors_are_left_alone(bits):
     gap = 512
     flat = [torch.full((sum(-(-n // BLOCK) * BLOCK + gap for n in sizes),), 7.0, device="cuda", dtype=dt)
             for dt in (torch.float32, torch.bfloat16, *((torch.float32,) * 2 if bits == 32 else (torch.uint8,) * 2))]
-    grads = torch.randn(flat[0].numel(), device="cuda")
+    grads = torch.randn(flat[0].numel(), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
     at, pieces = gap // 2, []
     for n in sizes:
         pieces.append((at, n))
@@ -270,7 +270,8 @@ def test_values_between_the_tensors_are_left_alone(bits):
         inside[a: a + n] = True
     for t in flat:
         assert (t[~inside] == 7).all()
-    assert (flat[0][inside] != 7).all()
+    # an update below half a step of 7.0 (2.4e-7 of lr = 1e-2: a new m below 2.4e-5 of its size, one in 10^4) leaves it as it is
+    assert (flat[0][inside] != 7).double().mean() > 0.99
 
 
 @pytest.mark.parametrize("bits", [32, 8])
