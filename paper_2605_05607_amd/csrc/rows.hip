@@ -31,6 +31,25 @@ constexpr int kRowsWaves = 4;  // tokens per workgroup: one per wave
 //   4096, all local, k = 2       2.8 / 3.3    4.5 / 4.9    6.3 / 6.0     8.6 / 7.7    18.6 / 16.8
 constexpr int kManyTokens = 1024;
 
+// The layout row (or -1) and the weight of slot `lane` of token t: the pick, its row and its weight are requested together.
+struct Slot {
+  int row;
+  float w;
+};
+__device__ __forceinline__ Slot slot_of_lane(const RowsArgs &a, int t, int lane) {
+  const int base = a.offsets[a.e_lo];
+  int e = -1, r = -1;
+  float w = 1.0f;
+  if (lane < a.k) {
+    const size_t at = (size_t)t * a.k + lane;
+    e = a.topk_idx[at];
+    r = a.inv_perm[at] - base;
+    if (a.topk_w) w = a.topk_w[at];
+  }
+  const bool local = e >= a.e_lo && e < a.e_lo + a.E_loc && r >= 0 && r < a.P_cap;
+  return {local ? r : -1, w};
+}
+
 // One wave per token and part of its columns (blockIdx.y of gridDim.y parts, taken in turn): PIECES pieces of 512 columns at a
 // time, and the loads of two slots in flight together.  STREAM: y leaves with the non-temporal hint.
 template <typename T, int PIECES, bool STREAM>
@@ -38,8 +57,7 @@ __global__ __launch_bounds__(kRowsWaves * 64) void combine_rows_kernel(const Row
   const int lane = threadIdx.x & 63;
   const int t = blockIdx.x * kRowsWaves + (threadIdx.x >> 6);  // wave-uniform
   if (t >= a.T) return;
-  const int row = combine_slot_row(a.topk_idx, a.inv_perm, t, a.k, lane, a.e_lo, a.E_loc, a.offsets[a.e_lo], a.P_cap);
-  const float w = row >= 0 && a.topk_w ? a.topk_w[(size_t)t * a.k + lane] : 1.0f;
+  const auto [row, w] = slot_of_lane(a, t, lane);
   const uint64_t slots = __ballot(row >= 0);
   T *out = static_cast<T *>(a.out) + (size_t)t * a.d;
   for (int c0 = lane * 8 + blockIdx.y * (512 * PIECES); c0 < a.d; c0 += 512 * PIECES * gridDim.y) {
@@ -92,8 +110,7 @@ __global__ __launch_bounds__(kBackThreads) void combine_rows_backward_kernel(con
   constexpr int WAVES = kBackThreads / 64;
   __shared__ float dots[WAVES][kMaxTopK];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = blockIdx.x;
-  const int row = combine_slot_row(a.topk_idx, a.inv_perm, t, a.k, lane, a.e_lo, a.E_loc, a.offsets[a.e_lo], a.P_cap);
-  const float w = row >= 0 ? a.topk_w[(size_t)t * a.k + lane] : 0.0f;
+  const auto [row, w] = slot_of_lane(a, t, lane);
   const T *dy = static_cast<const T *>(a.dy) + (size_t)t * a.d;
   if (lane < kMaxTopK) dots[wave][lane] = 0.f;
   for (uint64_t s = __ballot(row >= 0); s; s &= s - 1) {
