@@ -452,7 +452,8 @@ MOE355_API int moe_route_backward(const moe_shape *shape, const int32_t *topk_id
  *   sum: s as the forward wrote it (without a residual: x); rstd as the forward wrote it; dy [rows, cols]; dsum [rows, cols] the
  *   gradient that reaches s directly, down the residual stream (NULL: none); dx [rows, cols] the gradient of x and of the
  *   residual alike, it may be dy or dsum itself; dweight [cols] fp32 (NULL: not wanted, and no workspace needed), written in
- *   full.  Sums in fp32 in an order that depends on the sizes only: same inputs, same bits.  workspace >=
+ *   full.  Sums in fp32 in an order that depends on the sizes only (dweight's of up to 512 rows also on whether dx is dy): same
+ *   inputs, same bits.  workspace >=
  *   moe_rmsnorm_backward_workspace_bytes(rows, cols) (0 for invalid sizes), 16-byte aligned; a buffer for more rows serves fewer.
  */
 MOE355_API int moe_rmsnorm(int64_t rows, int cols, int dtype, const void *x, const void *residual, const void *weight,

@@ -167,11 +167,47 @@ struct NormBackArgs {
   const void *sum, *weight, *dy, *dsum;
   const float *rstd;
   void *dx;
-  float *partial;  // [workgroups][cols] sums of dy s rstd, null without the weight's gradient
+  float *partial;   // [workgroups][cols] sums of dy s rstd, null without the weight's gradient
+  float *direct;    // few rows: the weight's gradient itself, by the workgroups from `parts` on
+  int parts;        // workgroups that have rows
   int64_t rows;
   int cols;
   float inv_cols;
 };
+
+// The weight's gradient of few rows, straight from the rows (it needs nothing of dx): a workgroup has sixteen pieces of columns, its
+// threads take 32 rows at a time, and the 32 sums of a column are added in order.
+constexpr int kNormColumns = 16;  // pieces
+template <typename T, int THREADS>
+__device__ __forceinline__ void norm_weight_grad_columns(const NormBackArgs &a, int block, float *dweight) {
+  constexpr int N = Piece<T>::N, SUBS = THREADS / kNormColumns;
+  __shared__ float fold[SUBS][kNormColumns * N + 4];
+  const int sub = threadIdx.x / kNormColumns, piece = threadIdx.x % kNormColumns;
+  const int c = (block * kNormColumns + piece) * N;
+  float dw[N];
+#pragma unroll
+  for (int q = 0; q < N; ++q) dw[q] = 0.f;
+  if (c < a.cols) {
+#pragma unroll 4
+    for (int64_t row = sub; row < a.rows; row += SUBS) {
+      Piece<T> s, g;
+      s.load(static_cast<const T *>(a.sum) + row * a.cols + c);
+      g.load(static_cast<const T *>(a.dy) + row * a.cols + c);
+      const float rstd = a.rstd[row];
+#pragma unroll
+      for (int q = 0; q < N; ++q) dw[q] = fmaf(g.get(q) * s.get(q), rstd, dw[q]);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < N; ++q) fold[sub][piece * N + q] = dw[q];
+  __syncthreads();
+  const int mine = block * kNormColumns * N + threadIdx.x;
+  if (threadIdx.x >= kNormColumns * N || mine >= a.cols) return;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < SUBS; ++i) sum += fold[i][threadIdx.x];
+  dweight[mine] = sum;
+}
 
 // What a thread holds of a row.
 template <typename T, int CHUNKS>
@@ -214,6 +250,10 @@ __global__ __launch_bounds__(WAVES *GROUPS * 64) void rmsnorm_backward_kernel(co
   __shared__ float fold[GROUPS > 1 ? STRIDE : 1];
   // (the same in a wave: rows are addressed from scalar registers)
   const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (WAVES * 64)), t = threadIdx.x % (WAVES * 64);
+  if (blockIdx.x >= (unsigned)a.parts) {
+    norm_weight_grad_columns<T, WAVES * GROUPS * 64>(a, blockIdx.x - a.parts, a.direct);
+    return;
+  }
   const T *wt = static_cast<const T *>(a.weight);
   Piece<T> w[CHUNKS];
   float dw[CHUNKS][N];
@@ -224,7 +264,7 @@ __global__ __launch_bounds__(WAVES *GROUPS * 64) void rmsnorm_backward_kernel(co
 #pragma unroll
     for (int q = 0; q < N; ++q) dw[i][q] = 0.f;
   }
-  const int64_t step = (int64_t)gridDim.x * GROUPS;
+  const int64_t step = (int64_t)a.parts * GROUPS;
   int64_t row = (int64_t)blockIdx.x * GROUPS + group;
   NormBackRow<T, CHUNKS> now, next;
   now.load(a, row, t, STRIDE);
@@ -327,6 +367,11 @@ static void with_row_form(int64_t rows, int cols, F &&f) {
 constexpr int kNormBackWaves = 8, kNormParts = 256;
 constexpr int64_t kNormLaunchRows = 1 << 21;   // rows of one launch of the forward kernel
 
+// Up to here the weight's gradient comes from workgroups of the same launch that read s and dy again, beyond from partial rows and a
+// launch of its own (bf16, us, one launch and two: 64 x 7168 4.1 and 7.6, 255 x 2048 5.2 and 7.3, 512 x 7168 11.1 and 13.3, 512 x 512
+// 4.4 and 7.0, 1000 x 7168 20.2 and 18.5, 1000 x 512 8.0 and 8.4, 2000 x 2048 18.8 and 12.1).
+constexpr int kNormFewRows = 512;
+
 static int norm_check(int64_t rows, int cols, int dtype) {
   if (rows < 0 || rows > 0x7FFFFFFF || cols < 8 || cols % 8 != 0) return MOE_ERR_INVALID_ARG;
   if ((dtype != MOE_F32 && dtype != MOE_BF16) || cols > kNormMaxCols) return MOE_ERR_UNSUPPORTED;
@@ -359,13 +404,16 @@ static int norm_forward(NormArgs a, hipStream_t st) {
 }
 
 template <typename T>
-static int norm_backward(const NormBackArgs &a, float *dweight, hipStream_t st) {
-  int parts = 0;
+static int norm_backward(NormBackArgs a, float *dweight, hipStream_t st) {
+  const bool few = dweight && a.rows <= kNormFewRows && a.dx != a.dy;  // (there dy is read while dx is written)
+  if (few) a.partial = nullptr;
+  a.direct = few ? dweight : nullptr;
+  const int columns = few ? ceil_div(a.cols, kNormColumns * Piece<T>::N) : 0;
   const auto run = [&](auto waves, auto chunks, auto ahead) {
     constexpr int W = decltype(waves)::value, G = std::max(1, kNormBackWaves / W), C = decltype(chunks)::value;
-    parts = (int)std::min<int64_t>(kNormParts, (a.rows + G - 1) / G);
-    hipLaunchKernelGGL((rmsnorm_backward_kernel<T, W, C, G, decltype(ahead)::value>), dim3((unsigned)parts), dim3(W * G * 64), 0,
-                       st, a);
+    a.parts = (int)std::min<int64_t>(kNormParts, (a.rows + G - 1) / G);
+    hipLaunchKernelGGL((rmsnorm_backward_kernel<T, W, C, G, decltype(ahead)::value>), dim3((unsigned)(a.parts + columns)),
+                       dim3(W * G * 64), 0, st, a);
   };
   const std::integral_constant<int, 1> c1;
   const std::integral_constant<int, 2> c2;
@@ -381,8 +429,8 @@ static int norm_backward(const NormBackArgs &a, float *dweight, hipStream_t st) 
   else if (waves <= 32) run(c16, c4, std::false_type());
   else if constexpr (Piece<T>::N == 4) run(c16, c8, std::false_type());
   const int rc = launch_status();
-  if (rc != MOE_OK || !dweight) return rc;
-  hipLaunchKernelGGL(rmsnorm_weight_grad_kernel, dim3(ceil_div(a.cols, 64)), dim3(1024), 0, st, a.partial, parts, a.cols,
+  if (rc != MOE_OK || !dweight || few) return rc;
+  hipLaunchKernelGGL(rmsnorm_weight_grad_kernel, dim3(ceil_div(a.cols, 64)), dim3(1024), 0, st, a.partial, a.parts, a.cols,
                      dweight);
   return launch_status();
 }
@@ -433,7 +481,7 @@ extern "C" int moe_rmsnorm_backward(int64_t rows, int cols, int dtype, const voi
     hipLaunchKernelGGL(rmsnorm_zero_kernel, dim3(ceil_div(cols, 256)), dim3(256), 0, st, dweight, cols);
     return launch_status();
   }
-  NormBackArgs a{sum, weight, dy, dsum, rstd, dx, dweight ? static_cast<float *>(workspace) : nullptr, rows, cols,
+  NormBackArgs a{sum, weight, dy, dsum, rstd, dx, dweight ? static_cast<float *>(workspace) : nullptr, nullptr, 0, rows, cols,
                  1.0f / (float)cols};
   return dtype == MOE_BF16 ? norm_backward<bf16_t>(a, dweight, st) : norm_backward<float>(a, dweight, st);
 }

@@ -58,7 +58,7 @@ def check_codes(codes, scales, y, dt):
 
 
 # one wave, four and sixteen waves a row; every count of pieces a thread; columns that end inside a piece's wave; few rows
-SIZES = [(1, 8), (3, 8), (1, 7168), (2, 512), (5, 520), (300, 8), (257, 512), (301, 1000), (256, 2048), (259, 2056), (270, 2880),
+SIZES = [(1, 8), (3, 8), (1, 7168), (2, 512), (5, 520), (300, 8), (257, 512), (301, 1000), (256, 2048), (259, 2056), (270, 2880), (512, 136), (513, 136),
          (1025, 4096), (300, 7168), (256, 8192), (257, 8200), (3, 16384), (261, 16392), (2, 32768), (256, 32768), (4099, 264)]
 
 
@@ -106,7 +106,8 @@ def test_forward_and_gradients(rows, cols, dtype):
         size = (r * a).abs() + r ** 3 * s64.abs() * (a * s64).abs().mean(1, keepdim=True)
         assert ((dx.double() - ref_dx).abs() <= size * 2.0 ** -18 + ref_dx.abs() * (half(dt) + 4 * U)).all()
         # a column's sum: rows / (partial sums) in a register, eight registers, then 256 partial sums in sixteen chains
-        chain = rows / min(rows, 256) + 8 + 256 / 16 + 16
+        # (up to 512 rows: at most 16 rows in a register and 64 registers)
+        chain = max(rows / min(rows, 256) + 8 + 256 / 16 + 16, 80)
         assert ((dw.double() - ref_dw).abs() <= chain * U * (dy.double() * s64 * r).abs().sum(0) + 1e-300).all()
         # without the weight's gradient; into dy or the direct gradient itself; again: the same bits
         for target in (dy.clone(), None if direct is None else direct.clone()):
@@ -116,6 +117,11 @@ def test_forward_and_gradients(rows, cols, dtype):
             own_ds = direct if own_dy is target or direct is None else target
             B.moe_rmsnorm_backward(rows, cols, code, want_s, w, rstd, own_dy, own_ds, target, None, None)
             assert torch.equal(target, dx)
+        over = dy.clone()
+        B.moe_rmsnorm_backward(rows, cols, code, want_s, w, rstd, over, direct, over, dw, ws)
+        size = (dy.double() * s64 * r).abs().sum(0)
+        assert torch.equal(over, dx) and ((dw.double() - ref_dw).abs() <= chain * U * size + 1e-300).all()
+        B.moe_rmsnorm_backward(rows, cols, code, want_s, w, rstd, dy, direct, torch.empty_like(dx), dw, ws)
         again = torch.empty_like(dw)
         ws.fill_(0xFF)
         B.moe_rmsnorm_backward(rows, cols, code, want_s, w, rstd, dy, direct, torch.empty_like(dx), again, ws)
