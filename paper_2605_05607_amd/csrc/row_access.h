@@ -30,6 +30,12 @@ struct Row8 {
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = reinterpret_cast<const uint4 *>(p)[i];
   }
+  // with the non-temporal hint: what is read for the last time
+  __device__ __forceinline__ void load_last(const T *p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+      raw[i] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p) + i));
+  }
   __device__ __forceinline__ float get(int q) const {
     const uint4 r = raw[q * (int)sizeof(T) / 16];
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
