@@ -469,7 +469,7 @@ MOE355_API int moe_rmsnorm_backward(int64_t rows, int cols, int dtype, const voi
  * in the element type of the layer and not yet weighted.  rows, d_rows, d_xs [P_cap, d] (layout rows as moe_dispatch_gather
  * writes them), dy, y, dx [T, d]; pointers 16-byte aligned; topk_idx, topk_w, tables of the batch (perm and the rank arrays are not
  * read).  Sums in fp32 in slot order, one rounding at the write; what lies behind the last local row is neither read nor written.
- * T < 2^24 (MOE_ERR_UNSUPPORTED otherwise).
+ * T < 2^24, d <= 2^30 (MOE_ERR_UNSUPPORTED otherwise).
  *
  * moe_combine_weighted: y[t] = sum over the local slots j of topk_w[t,j] rows[row of (t,j)], zeros where there is none.
  * moe_combine_weighted_backward: d_rows[row of (t,j)] = topk_w[t,j] dy[t], d_topk_w[t,j] = <rows[row of (t,j)], dy[t]> in fp32
@@ -502,7 +502,7 @@ MOE355_API int moe_dispatch_gather_backward(const moe_shape *shape, const void *
  * The step's own numbers, moe_adamw_device: step counts from 1.  They come from config->now, or, where `device` is not NULL, from
  * that device memory when the kernels run (for captured steps: write it between replays; lr and step are then not checked).
  * A grad_scale that is not finite leaves every array as it was (a step whose gradients have overflowed is skipped without a
- * word from the host).  Same inputs, same bits.
+ * word from the host).  Same inputs, same bits; the states' fp32 operations are rounded one by one.
  */
 #define MOE_ADAMW_BLOCK 256
 typedef struct {

@@ -56,6 +56,33 @@ struct AdamStep {
   float beta1, beta2, new1, new2, eps, keep, rate, root2, grad_scale;
 };
 
+// 1 - b^t for x = t log b, without the cancellation of small t: the exponential's series up to the eighth power (x > -1/2: what is
+// left out is below 2^-26 of the result), else the difference.
+__device__ __forceinline__ float one_less_power(float x) {
+  float p = 1.0f / 40320;
+  p = fmaf(p, x, 1.0f / 5040);
+  p = fmaf(p, x, 1.0f / 720);
+  p = fmaf(p, x, 1.0f / 120);
+  p = fmaf(p, x, 1.0f / 24);
+  p = fmaf(p, x, 1.0f / 6);
+  p = fmaf(p, x, 0.5f);
+  p = fmaf(p, x, 1.0f);
+  return x > -0.5f ? -x * p : 1.0f - __expf(x);
+}
+__device__ __forceinline__ AdamStep step_numbers(const AdamArgs &a, const moe_adamw_device &now, const AdamTensor &x) {
+  AdamStep s;
+  s.beta1 = a.beta1;
+  s.beta2 = a.beta2;
+  s.new1 = a.new1;
+  s.new2 = a.new2;
+  s.eps = a.eps;
+  s.keep = 1.0f - now.lr * x.weight_decay;
+  s.rate = now.lr / one_less_power((float)now.step * a.log_beta1);
+  s.root2 = 1.0f / sqrtf(one_less_power((float)now.step * a.log_beta2));
+  s.grad_scale = now.grad_scale;
+  return s;
+}
+
 // New m, v, sqrt(v) and parameter of one element.  The states' operations round one by one (no contraction, the correctly
 // rounded square root): where a state is held in codes, the last bit of a value can decide which code it gets, and this way the
 // codes are those of the formulas evaluated in fp32 by anyone.
@@ -261,39 +288,49 @@ struct AdamQuad {
   }
 };
 
-// PER blocks of 256 values for a wave, a workgroup's waves side by side.  Whole chunks are read before the first block is worked on.
-// 32-bit states: two.  8-bit states, whose blocks take 300 vector instructions each: four where a launch has the values to fill the
-// chip with that, else one (bf16 gradients and copies, 2^17 / 2^19 / 2^21 / 2^23 / 2^25 values: one block 4.4, 5.3, 12.6, 34.0 and
-// 115.8 us, two 5.1, 5.5, 12.9, 32.6 and 108.2, four 6.8, 7.3, 14.1, 32.9 and 105.4).
-constexpr int kAdamFew = 1 << 21;
+// PER blocks of 256 values for a wave, a workgroup's waves side by side; all are requested before the first is worked on.  32-bit
+// states: two.  8-bit states, whose blocks take 350 vector instructions each: four where a launch has the values to fill the chip
+// with that, else one (bf16 gradients and copies, 2^18 / 2^20 / 2^22 / 2^24 / 2^25 values: one block 3.7, 6.6, 16.7, 53.1 and 100.8 us,
+// four 6.4, 8.1, 17.6, 50.2 and 92.0).
+constexpr int kAdamFew = 1 << 22;
 constexpr int64_t adam_chunk_values(int per) { return (int64_t)per * kAdamThreads * 4; }
 template <bool EIGHT, bool BF16, int PER>
-__device__ __forceinline__ void adam_chunk(const AdamTensor &x, const AdamStep &s, int64_t begin, uint32_t key) {
-  constexpr int64_t CHUNK = adam_chunk_values(PER);
+__device__ __forceinline__ void adam_chunk(const AdamArgs &a, const moe_adamw_device &now, const AdamTensor &x, int64_t begin,
+                                           uint32_t key) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t first = begin + wave * kAdamBlock;
+  constexpr int NEXT = kAdamThreads * 4;  // from a wave's block to its next one
   AdamQuad<EIGHT, BF16> quad[PER];
-  if (begin + CHUNK <= x.n) {
+  if (PER > 1 && begin + adam_chunk_values(PER) <= x.n) {
+#pragma unroll
+    for (int b = 0; b < PER; ++b) quad[b].load(x, first + b * NEXT + lane * 4, (first + b * NEXT) / kAdamBlock);
+    const AdamStep s = step_numbers(a, now, x);  // (while they are on their way)
 #pragma unroll
     for (int b = 0; b < PER; ++b) {
-      const int64_t at = first + b * (kAdamThreads * 4);
-      quad[b].load(x, at + lane * 4, at / kAdamBlock);
-    }
-#pragma unroll
-    for (int b = 0; b < PER; ++b) {
-      const int64_t at = first + b * (kAdamThreads * 4);
-      quad[b].step(s, x, at + lane * 4, at / kAdamBlock, key);
-      quad[b].store(x, at + lane * 4);
+      quad[b].step(s, x, first + b * NEXT + lane * 4, (first + b * NEXT) / kAdamBlock, key);
+      quad[b].store(x, first + b * NEXT + lane * 4);
     }
     return;
   }
-  for (int64_t at = first; at < min(x.n, begin + CHUNK); at += kAdamThreads * 4) {  // (the same in a wave)
-    const int64_t i = at + lane * 4;
-    const int here = (int)max((int64_t)0, min((int64_t)4, x.n - i));
-    AdamQuad<EIGHT, BF16> one;
-    if (here == 4) one.load(x, i, at / kAdamBlock); else one.load(x, i, at / kAdamBlock, here);
-    one.step(s, x, i, at / kAdamBlock, key);
-    if (here == 4) one.store(x, i); else one.store(x, i, here);
+#pragma unroll
+  for (int b = 0; b < PER; ++b) {
+    const int64_t at = first + b * NEXT;  // (the same in a wave)
+    if (at + kAdamBlock <= x.n) quad[b].load(x, at + lane * 4, at / kAdamBlock);
+  }
+  const AdamStep s = step_numbers(a, now, x);
+#pragma unroll
+  for (int b = 0; b < PER; ++b) {
+    const int64_t at = first + b * NEXT, i = at + lane * 4;
+    if (at + kAdamBlock <= x.n) {
+      quad[b].step(s, x, i, at / kAdamBlock, key);
+      quad[b].store(x, i);
+    } else if (at < x.n) {  // the tensor's last block
+      const int here = (int)max((int64_t)0, min((int64_t)4, x.n - i));
+      AdamQuad<EIGHT, BF16> one;
+      if (here == 4) one.load(x, i, at / kAdamBlock); else one.load(x, i, at / kAdamBlock, here);
+      one.step(s, x, i, at / kAdamBlock, key);
+      if (here == 4) one.store(x, i); else one.store(x, i, here);
+    }
   }
 }
 
@@ -306,19 +343,9 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
   const int k = __builtin_amdgcn_readfirstlane(
       (int)__popcll(__ballot(lane + 1 < a.count && blockIdx.x >= a.first[min(lane + 1, kAdamTensors)])));
   const AdamTensor &x = a.tensor[k];
-  AdamStep s;
-  s.beta1 = a.beta1;
-  s.beta2 = a.beta2;
-  s.new1 = a.new1;
-  s.new2 = a.new2;
-  s.eps = a.eps;
-  s.keep = 1.0f - now.lr * x.weight_decay;
-  s.rate = now.lr / -expm1f((float)now.step * a.log_beta1);  // (1 - b^t without the cancellation)
-  s.root2 = 1.0f / sqrtf(-expm1f((float)now.step * a.log_beta2));
-  s.grad_scale = now.grad_scale;
   const int64_t begin = (int64_t)(blockIdx.x - a.first[k]) * adam_chunk_values(PER);
   const uint32_t key = EIGHT ? mix(now.seed + mix((uint32_t)now.step + mix((uint32_t)(a.index0 + k) + 0x9E3779B9u))) : 0u;
-  if (x.grad_bf16) adam_chunk<EIGHT, true, PER>(x, s, begin, key); else adam_chunk<EIGHT, false, PER>(x, s, begin, key);
+  if (x.grad_bf16) adam_chunk<EIGHT, true, PER>(a, now, x, begin, key); else adam_chunk<EIGHT, false, PER>(a, now, x, begin, key);
 }
 
 }  // namespace moe355

@@ -149,6 +149,7 @@ __global__ __launch_bounds__(kBackThreads) void combine_rows_backward_kernel(con
 }
 
 constexpr int kMostTokens = 1 << 24;  // a workgroup of 256 threads for each, and a grid's threads are counted in 32 bits
+constexpr int kMostColumns = 1 << 30;  // (column indexes run past the end by up to 2^27)
 static bool tables_there(const moe_dispatch *tb) { return tb && tb->offsets && tb->inv_perm; }
 static bool off16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 != 0; }
 
@@ -159,7 +160,7 @@ static int combine_rows(const moe_shape *shape, const void *rows, const int32_t 
   if (rc != MOE_OK) return rc;
   if (!rows || !topk_idx || !tables_there(tables) || !out) return MOE_ERR_INVALID_ARG;
   if (off16(rows) || off16(out) || rows == out) return MOE_ERR_INVALID_ARG;
-  if (shape->T >= kMostTokens) return MOE_ERR_UNSUPPORTED;
+  if (shape->T >= kMostTokens || shape->d > kMostColumns) return MOE_ERR_UNSUPPORTED;
   if (shape->T == 0) return MOE_OK;
   RowsArgs a{rows, nullptr, topk_idx, tables->inv_perm, tables->offsets, topk_w, out, nullptr,
              shape->T, shape->k, shape->d, dv.e_lo, dv.E_loc, (int)dv.P_cap};
@@ -203,7 +204,7 @@ extern "C" int moe_combine_weighted_backward(const moe_shape *shape, const void 
   if (rc != MOE_OK) return rc;
   if (!rows || !dy || !topk_idx || !topk_w || !tables_there(tables) || !d_rows || !d_topk_w) return MOE_ERR_INVALID_ARG;
   if (off16(rows) || off16(dy) || off16(d_rows) || d_rows == dy) return MOE_ERR_INVALID_ARG;
-  if (shape->T >= kMostTokens) return MOE_ERR_UNSUPPORTED;
+  if (shape->T >= kMostTokens || shape->d > kMostColumns) return MOE_ERR_UNSUPPORTED;
   if (shape->T == 0) return MOE_OK;
   RowsArgs a{rows, dy, topk_idx, tables->inv_perm, tables->offsets, topk_w, d_rows, d_topk_w,
              shape->T, shape->k, shape->d, dv.e_lo, dv.E_loc, (int)dv.P_cap};

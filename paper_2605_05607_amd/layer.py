@@ -90,7 +90,7 @@ class MoELayer:
 
     def norm(self, h, residual=None, codes: bool = False) -> None:
         """x (and, for forward_fp8_codes, its codes) from the output h of what comes before the layer; with a residual the new
-        one is left in ``norm_sum``."""
+        one is left in ``norm_sum``.  norm_backward reads that (without a residual h) again."""
         self._normed = h if residual is None else self.norm_sum
         B.moe_rmsnorm(self.shape.T, self.shape.d, self.shape.dtype, h, residual, self.norm_weight, self.norm_eps,
                       None if residual is None else self.norm_sum, self.x, self.x_codes if codes else None,
@@ -229,6 +229,9 @@ class AdamW:
             for t, dtype, size in held:
                 if t is None or t.dtype != dtype or t.numel() != size or not t.is_contiguous() or t.device != params[0].device:
                     raise ValueError("contiguous tensors of the parameter's size on one device: fp32 parameters, bf16 copies")
+        written = [t.data_ptr() for t in (*params, *copies, *(t for s in states for t in s)) if t is not None and t.numel()]
+        if len(set(written)) < len(written):
+            raise ValueError("a tensor that a step writes is there twice")
         self.params, self.grads, self.copies, self.states = list(params), list(grads), copies, states
         self.steps = steps
         self.config = B.moe_adamw_config(beta1, beta2, eps, bits, B.moe_adamw_device(lr, 1.0, 0, seed))
@@ -243,10 +246,16 @@ class AdamW:
             self._count = self.scalars[2:3]
 
     def step(self, lr=None, grad_scale=1.0) -> None:
-        """One step with the gradients as they are.  lr: a new rate from now on.  With device scalars both are set there."""
+        """One step with the gradients as they are.  lr: a new rate from now on.  grad_scale: multiplies the gradients; one that is
+        not finite skips the step, which counts all the same.  With device scalars both are set there."""
         if self.scalars is not None:
             if lr is not None or grad_scale != 1.0:
                 raise ValueError("lr and grad_scale are in `scalars`")
+        import torch
+        if self.params and self.params[0].device.index != torch.cuda.current_device():
+            with torch.cuda.device(self.params[0].device):
+                return self.step(lr, grad_scale)
+        if self.scalars is not None:
             self._count += 1
         elif lr is not None:
             self.config.now.lr = lr

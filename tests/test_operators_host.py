@@ -75,6 +75,7 @@ def test_rows_refusals():
     assert rows_calls(good_shape(T=0), out=A) == (INV, 0, INV)  # (d_rows may be rows)
     assert rows_calls(good_shape(T=0), out=2 * A) == (0, INV, 0)
     assert rows_calls(good_shape(T=0)) == (0, 0, 0) and rows_calls(good_shape(T=1 << 24)) == (UNS,) * 3
+    assert rows_calls(good_shape(d=(1 << 30) + 8)) == (UNS,) * 3
 
 
 def adamw(tensor=None, device=None, count=1, **config):
@@ -109,7 +110,8 @@ def test_adamw_class_checks_its_tensors():
     for args, kw in ((([p], []), {}), (([p.bfloat16()], [g]), {}), (([p], [g[:5]]), {}), (([p], [g.half()]), {}),
                      (([p], [g]), dict(copies=[p])), (([p], [g]), dict(bits=16)), (([p], [g]), dict(weight_decay=[0.1, 0.1])),
                      (([torch.zeros(4, 4).t()[:2]], [torch.zeros(8)]), {}),
-                     (([p], [g]), dict(bits=8, states=[(p, p, None, None)]))):
+                     (([p], [g]), dict(bits=8, states=[(p, p, None, None)])), (([p, p], [g, g]), {}),
+                     (([p], [g]), dict(states=[(p, torch.zeros(10), None, None)]))):
         with pytest.raises((ValueError, AttributeError)):
             L.AdamW(*args, 1e-3, **kw)
     opt = L.AdamW([p], [g], 1e-3, bits=8, seed=0xFFFFFFFF, device_scalars=True)
