@@ -140,6 +140,30 @@ def test_steps_against_float64(sizes, bits):
                     check_state(codes, scale, value, 16 * U * value if least else tol_m, rnd, least)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gradients_and_copies_of_both_kinds_in_one_list(bits):
+    """Each tensor gets what it gets in a list of its own kind (32 bits), or at its own place of the list (8: the hash)."""
+    sizes = [700, 4097, 256, 9000, 0, 31]
+    sets = []
+    for kinds in (("b", "f", "b", "f", "f", "b"), "bbbbbb", "ffffff"):
+        params, grads, _, states = make(sizes, bits, torch.bfloat16, False, 12)
+        grads = [g if k == "b" else g.float() for g, k in zip(grads, kinds)]  # (the same values)
+        copies = [torch.zeros(n, dtype=torch.bfloat16, device="cuda") if k == "b" else None for n, k in zip(sizes, kinds)]
+        L.AdamW(params, grads, 1e-3, copies=copies, bits=bits, states=states, steps=5, seed=2).step()
+        assert all(c is None or torch.equal(c, p.bfloat16()) for c, p in zip(copies, params))
+        sets.append(params + [t for s in states for t in s if t is not None])
+    for other in sets[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(sets[0], other))
+
+
+def test_lists_without_values():
+    L.AdamW([], [], 1e-3).step()
+    for bits in (32, 8):
+        p = torch.zeros(0, device="cuda")
+        L.AdamW([p], [p], 1e-3, bits=bits).step()
+    torch.cuda.synchronize()
+
+
 def test_rounding_has_no_bias():
     """Values between two codes: the mean of what is held is the value.  n draws of a part f of a step d: standard deviation
     d sqrt(f (1 - f) / n), and the 16 bits are off by at most d 2^-16."""

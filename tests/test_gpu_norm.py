@@ -243,6 +243,53 @@ def test_replays_from_a_graph_on_another_stream():
             assert torch.equal(a, b), turn
 
 
+def test_rows_of_several_launches():
+    rows, cols = (1 << 21) + 5, 8
+    x, res, w, dy, _ = inputs(rows, cols, torch.bfloat16, 13)
+    s, y, q = torch.empty_like(x), torch.empty_like(x), torch.empty((rows, cols), dtype=torch.uint8, device="cuda")
+    sc, rstd = (torch.full((rows,), 7.0, device="cuda") for _ in range(2))
+    B.moe_rmsnorm(rows, cols, B.MOE_BF16, x, res, w, EPS, s, y, q, sc, rstd)
+    assert torch.equal(s, (x.float() + res.float()).bfloat16())
+    ref, r64 = forward64(s, w)
+    assert ((rstd.double() - r64).abs() <= r64 * 2.0 ** -18).all()
+    assert ((y.double() - ref).abs() <= ref.abs() * (half(torch.bfloat16) + 2.0 ** -18)).all()
+    check_codes(q, sc, ref, torch.bfloat16)
+    dx, dw = torch.empty_like(x), torch.empty(cols, device="cuda")
+    ws = torch.empty(B.moe_rmsnorm_backward_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    B.moe_rmsnorm_backward(rows, cols, B.MOE_BF16, s, w, rstd, dy, None, dx, dw, ws)
+    ref_dx, ref_dw = backward64(s, w, rstd, dy, None)
+    assert (dx.double() - ref_dx).abs().max() <= 2.0 ** -7 * ref_dx.abs().max()
+    # a chain of rows / 256 / 8 in a register
+    size = (dy.double() * s.double() * rstd.double()[:, None]).abs().sum(0)
+    assert ((dw.double() - ref_dw).abs() <= (rows / 2048 + 64) * U * size).all()
+
+
+def test_two_streams_at_once():
+    rows, cols = 900, 4096
+    sets = [inputs(rows, cols, torch.bfloat16, 40 + i) for i in range(2)]
+
+    def call(a, ws):
+        x, res, w, dy, dsum = a
+        s, y, dx = (torch.empty_like(x) for _ in range(3))
+        rstd, dw = torch.empty(rows, device="cuda"), torch.empty(cols, device="cuda")
+        for _ in range(5):
+            B.moe_rmsnorm(rows, cols, B.MOE_BF16, x, res, w, EPS, s, y, None, None, rstd)
+            B.moe_rmsnorm_backward(rows, cols, B.MOE_BF16, s, w, rstd, dy, dsum, dx, dw, ws)
+        return s, y, dx, rstd, dw
+    size = B.moe_rmsnorm_backward_workspace_bytes(rows, cols)
+    spaces = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    want = [call(a, ws) for a, ws in zip(sets, spaces)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for a, ws, st in zip(sets, spaces, streams):
+        with torch.cuda.stream(st):
+            got.append(call(a, ws))
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(p, q) for p, q in zip(g, w))
+
+
 def test_more_than_2_to_the_31_values():
     rows, cols = 65600, 32768  # 2.15e9 values: offsets past 32 bits
     x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")

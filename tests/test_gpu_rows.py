@@ -71,12 +71,17 @@ def test_back_and_gradients(shape, dtype):
     T, d, E, k, R, lo, hi, router = shape
     b = Batch(T, d, E, k, R, lo, hi, dtype, router)
     picks = b.idx[: T * k].clone()
-    for form in ("as routed", "picks outside", "no local row"):
+    for form in ("as routed", "picks outside", "one expert twice", "no local row"):
+        if form == "one expert twice" and k > b.lay.cfg.E_loc:
+            continue  # (more rows than picks of distinct experts have room for)
         if form != "as routed":
             p = picks.view(T, k).clone()
             if form == "picks outside":
                 p[1::3] = -1
                 p[2::3, 0] = E + 5
+            elif form == "one expert twice":
+                p[:, -1] = p[:, 0]
+                p[::4] = b.lay.cfg.first_local_expert
             else:
                 p[:] = (b.lay.cfg.first_local_expert + b.lay.cfg.E_loc) % E if b.lay.cfg.E_loc < E else -1
             b.idx[: T * k].copy_(p.view(-1))
