@@ -249,11 +249,34 @@ struct NormBackRow {
   }
 };
 
+// The sums over a piece, and its part of dx.
+template <typename T>
+__device__ __forceinline__ float norm_back_sums(const Piece<T> &s, const Piece<T> &g, const Piece<T> &w, float rstd, float dot,
+                                                float (&dw)[Piece<T>::N]) {
+#pragma unroll
+  for (int q = 0; q < Piece<T>::N; ++q) {
+    const float gs = g.get(q) * s.get(q);
+    dot = fmaf(gs, w.get(q), dot);
+    dw[q] = fmaf(gs, rstd, dw[q]);
+  }
+  return dot;
+}
+template <typename T>
+__device__ __forceinline__ void norm_back_store(const Piece<T> &s, const Piece<T> &g, const Piece<T> &w, const Piece<T> &r,
+                                                float rstd, float mean, T *dst) {
+  float o[Piece<T>::N];
+#pragma unroll
+  for (int q = 0; q < Piece<T>::N; ++q) o[q] = fmaf(rstd, fmaf(-mean, s.get(q), g.get(q) * w.get(q)), r.get(q));
+  *reinterpret_cast<uint4 *>(dst) = Piece<T>::pack(o);
+}
+
 // Rows in turn, GROUPS of them at a time (WAVES waves each), the next ones on their way while the sum over a row is formed.  The
 // threads' columns are the same in every row, so the weight's gradient is summed in registers; a workgroup writes one partial row.
 // With the sum over those: 8192 x 4096 in bf16 with dsum 47 us, 5.7 TB/s; 4096 x 7168 45 us, 5.3.  FEW: workgroups from `parts` on
-// form the weight's gradient instead.
-template <typename T, int WAVES, int CHUNKS, int GROUPS, bool AHEAD, bool FEW>
+// form the weight's gradient instead.  Not HELD: rows of more than 32 KiB are read a second time behind their sum, from the caches, and
+// none ahead (2048 x 32768 in bf16 134 us, 4.0 TB/s; held in registers, which
+// do not suffice, 360).
+template <typename T, int WAVES, int CHUNKS, int GROUPS, bool HELD, bool FEW>
 __global__ __launch_bounds__(WAVES *GROUPS * 64) void rmsnorm_backward_kernel(const NormBackArgs a) {
   constexpr int N = Piece<T>::N, STRIDE = WAVES * 64 * N;
   __shared__ float sums[2][WAVES * GROUPS];
@@ -276,34 +299,53 @@ __global__ __launch_bounds__(WAVES *GROUPS * 64) void rmsnorm_backward_kernel(co
   }
   const int64_t step = (int64_t)a.parts * GROUPS;
   int64_t row = (int64_t)blockIdx.x * GROUPS + group;
-  NormBackRow<T, CHUNKS, !FEW> now, next;
-  now.load(a, row, t, STRIDE);
   int turn = 0;
-  for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < a.rows; first += step, row += step, turn ^= 1) {
-    if constexpr (AHEAD) next.load(a, row + step, t, STRIDE);
-    float dot = 0.f;
+  if constexpr (HELD) {
+    NormBackRow<T, CHUNKS, !FEW> now, next;
+    now.load(a, row, t, STRIDE);
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < a.rows; first += step, row += step, turn ^= 1) {
+      next.load(a, row + step, t, STRIDE);
+      float dot = 0.f;
 #pragma unroll
-    for (int i = 0; i < CHUNKS; ++i)
+      for (int i = 0; i < CHUNKS; ++i) dot = norm_back_sums<T>(now.s[i], now.g[i], w[i], now.rstd, dot, dw[i]);
+      dot = row_reduce<WAVES>(dot, sums[turn], AddF());
+      now.pin();
+      const float mean = dot * a.inv_cols * now.rstd * now.rstd;
 #pragma unroll
-      for (int q = 0; q < N; ++q) {
-        const float gs = now.g[i].get(q) * now.s[i].get(q);
-        dot = fmaf(gs, w[i].get(q), dot);
-        dw[i][q] = fmaf(gs, now.rstd, dw[i][q]);
+      for (int i = 0; i < CHUNKS; ++i) {
+        const int c = t * N + i * STRIDE;
+        if (row < a.rows && c < a.cols)
+          norm_back_store<T>(now.s[i], now.g[i], w[i], now.r[i], now.rstd, mean, static_cast<T *>(a.dx) + row * a.cols + c);
       }
-    dot = row_reduce<WAVES>(dot, sums[turn], AddF());
-    if constexpr (AHEAD) now.pin();
-    const float mean = dot * a.inv_cols * now.rstd * now.rstd;
-#pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
-      const int c = t * N + i * STRIDE;
-      if (row >= a.rows || c >= a.cols) continue;
-      float o[N];
-#pragma unroll
-      for (int q = 0; q < N; ++q)
-        o[q] = fmaf(now.rstd, fmaf(-mean, now.s[i].get(q), now.g[i].get(q) * w[i].get(q)), now.r[i].get(q));
-      *reinterpret_cast<uint4 *>(static_cast<T *>(a.dx) + row * a.cols + c) = Piece<T>::pack(o);
+      now = next;
     }
-    if constexpr (AHEAD) now = next; else now.load(a, row + step, t, STRIDE);
+  } else {  // (one group: the row is there)
+    for (; row < a.rows; row += step, turn ^= 1) {
+      const int64_t base = row * a.cols;
+      const float rstd = a.rstd[row];
+      float dot = 0.f;
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i) {
+        const int c = t * N + i * STRIDE;
+        Piece<T> s, g;
+        if (c >= a.cols) continue;
+        s.load(static_cast<const T *>(a.sum) + base + c);
+        g.load(static_cast<const T *>(a.dy) + base + c);
+        dot = norm_back_sums<T>(s, g, w[i], rstd, dot, dw[i]);
+      }
+      dot = row_reduce<WAVES>(dot, sums[turn], AddF());
+      const float mean = dot * a.inv_cols * rstd * rstd;
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i) {
+        const int c = t * N + i * STRIDE;
+        Piece<T> s, g, r;
+        if (c >= a.cols) continue;
+        s.load(static_cast<const T *>(a.sum) + base + c);
+        g.load(static_cast<const T *>(a.dy) + base + c);
+        if (a.dsum) r.load_last(static_cast<const T *>(a.dsum) + base + c); else r.zero();
+        norm_back_store<T>(s, g, w[i], r, rstd, mean, static_cast<T *>(a.dx) + base + c);
+      }
+    }
   }
   if (FEW || !a.partial) return;
 #pragma unroll
@@ -419,15 +461,15 @@ static int norm_backward(NormBackArgs a, float *dweight, hipStream_t st) {
   if (few) a.partial = nullptr;
   a.direct = few ? dweight : nullptr;
   const int columns = few ? ceil_div(a.cols, kNormColumns * Piece<T>::N) : 0;
-  const auto run = [&](auto waves, auto chunks, auto ahead) {
+  const auto run = [&](auto waves, auto chunks, auto held) {
     constexpr int W = decltype(waves)::value, G = std::max(1, kNormBackWaves / W), C = decltype(chunks)::value;
     a.parts = (int)std::min<int64_t>(kNormParts, (a.rows + G - 1) / G);
-    constexpr bool AHEAD = decltype(ahead)::value;
+    constexpr bool HELD = decltype(held)::value;
     const dim3 grid((unsigned)(a.parts + columns)), block(W * G * 64);
     if (few)
-      hipLaunchKernelGGL((rmsnorm_backward_kernel<T, W, C, G, AHEAD, true>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((rmsnorm_backward_kernel<T, W, C, G, HELD, true>), grid, block, 0, st, a);
     else
-      hipLaunchKernelGGL((rmsnorm_backward_kernel<T, W, C, G, AHEAD, false>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((rmsnorm_backward_kernel<T, W, C, G, HELD, false>), grid, block, 0, st, a);
   };
   const std::integral_constant<int, 1> c1;
   const std::integral_constant<int, 2> c2;
