@@ -274,8 +274,7 @@ __device__ __forceinline__ void norm_back_store(const Piece<T> &s, const Piece<T
 // threads' columns are the same in every row, so the weight's gradient is summed in registers; a workgroup writes one partial row.
 // With the sum over those: 8192 x 4096 in bf16 with dsum 47 us, 5.7 TB/s; 4096 x 7168 45 us, 5.3.  FEW: workgroups from `parts` on
 // form the weight's gradient instead.  Not HELD: rows of more than 32 KiB are read a second time behind their sum, from the caches, and
-// none ahead (2048 x 32768 in bf16 134 us, 4.0 TB/s; held in registers, which
-// do not suffice, 360).
+// none ahead (2048 x 32768 in bf16 134 us, 4.0 TB/s; held in registers, which do not suffice, 360).
 template <typename T, int WAVES, int CHUNKS, int GROUPS, bool HELD, bool FEW>
 __global__ __launch_bounds__(WAVES *GROUPS * 64) void rmsnorm_backward_kernel(const NormBackArgs a) {
   constexpr int N = Piece<T>::N, STRIDE = WAVES * 64 * N;

@@ -116,7 +116,6 @@ __global__ __launch_bounds__(kBackThreads) void combine_rows_backward_kernel(con
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = blockIdx.x;
   const auto [row, w] = slot_of_lane(a, t, lane);
   const T *dy = static_cast<const T *>(a.dy) + (size_t)t * a.d;
-  if (lane < kMaxTopK) dots[wave][lane] = 0.f;
   for (uint64_t s = __ballot(row >= 0); s; s &= s - 1) {
     const int j = __builtin_ctzll(s);
     const float wj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j));
@@ -142,9 +141,11 @@ __global__ __launch_bounds__(kBackThreads) void combine_rows_backward_kernel(con
   }
   __syncthreads();
   if (threadIdx.x >= (unsigned)a.k) return;
-  float dot = 0.f;  // (a slot that is not local has zeros)
+  float dot = 0.f;
+  if (row >= 0) {  // (thread j has slot j)
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) dot += dots[i][threadIdx.x];
+    for (int i = 0; i < WAVES; ++i) dot += dots[i][threadIdx.x];
+  }
   a.d_w[(size_t)t * a.k + threadIdx.x] = dot;
 }
 
