@@ -24,11 +24,11 @@ struct RowsArgs {
 constexpr int kRowsWaves = 4;  // tokens per workgroup: one per wave
 // Above, a wave takes four pieces of 512 columns (fp32: two; 8192 x 4096 62.6 us against 68.5) and y leaves with the non-temporal hint; up to here one piece, so that there are
 // waves enough, and plain stores.  Microseconds of the two forms (few / many), bf16:
-//   tokens                       64           512          1024         1536          3072
-//   7168, 1 of 8 ranks, k = 8    3.0 / 4.0    5.2 / 5.5    7.1 / 7.3    11.9 / 9.2    22.3 / 18.3
-//   2880, 1 of 4, k = 4          2.8 / 3.4    3.4 / 4.0    4.7 / 4.8     6.0 / 5.6     8.6 / 8.3
-//   2048, 1 of 8, k = 8          2.7 / 3.6    3.1 / 4.0    3.9 / 4.5     4.6 / 5.1     6.8 / 6.9
-//   4096, all local, k = 2       2.8 / 3.3    4.5 / 4.9    6.3 / 6.0     8.6 / 7.7    18.6 / 16.8
+//   tokens                       64           512          1024         1536          3000
+//   7168, 1 of 8 ranks, k = 8    2.8 / 3.5    5.1 / 5.2    6.7 / 7.0    11.3 / 9.1    21.3 / 18.3
+//   2880, 1 of 4, k = 4          2.7 / 3.4    3.3 / 3.7    4.7 / 4.7     5.7 / 5.4     8.0 / 7.6
+//   2048, 1 of 8, k = 8          2.6 / 3.4    3.0 / 3.6    3.7 / 4.2     4.5 / 4.9     6.4 / 6.1
+//   4096, all local, k = 2       2.6 / 3.2    4.4 / 4.7    5.9 / 5.9     8.7 / 7.3    17.7 / 15.5
 constexpr int kManyTokens = 1024;
 
 // The layout row (or -1) and the weight of slot `lane` of token t: the pick, its row and its weight are requested together.
