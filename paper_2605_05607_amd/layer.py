@@ -125,9 +125,11 @@ class MoELayer:
             self.dW_gate = self.dW_up = self.dW_down = None
 
     def enable_optimizer(self, W_gate: np.ndarray, W_up: np.ndarray, W_down: np.ndarray, lr: float, **kw) -> None:
-        """An AdamW step on the three expert weights, after enable_training: fp32 parameters, bf16 copies of them and the
-        optimizer (`kw` as for AdamW)."""
+        """An AdamW step on the three expert weights, after enable_training with weight gradients: fp32 parameters, bf16 copies of
+        them and the optimizer (`kw` as for AdamW)."""
         import torch
+        if getattr(self, "dW_gate", None) is None:
+            raise ValueError("enable_training with weight gradients comes first")
         self.weights = [to_device(a, self.device) for a in (W_gate, W_up, W_down)]
         self.masters = [w.to(torch.float32) for w in self.weights]
         self.optimizer = AdamW(self.masters, [self.dW_gate, self.dW_up, self.dW_down], lr, copies=self.weights, **kw)

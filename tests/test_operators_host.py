@@ -118,3 +118,18 @@ def test_adamw_class_checks_its_tensors():
     assert opt.scalars.tolist()[2:] == [0, -1] and opt.states[0][2].numel() == 1
     with pytest.raises(ValueError):
         opt.step(lr=1.0)
+
+
+def test_layer_asks_for_what_comes_first():
+    import torch
+
+    from paper_2605_05607_amd import layer as L
+    from paper_2605_05607_amd import workloads as wl
+    lay = L.MoELayer(wl.CONFIGS["tiny"].scaled(T=4, dtype=wl.BF16), device="cpu")
+    with pytest.raises(ValueError):
+        lay.enable_optimizer(None, None, None, 1e-3)
+    for w in (torch.ones(512), torch.ones(504, dtype=torch.bfloat16)):
+        with pytest.raises(ValueError):
+            lay.enable_norm(w)
+    lay.enable_norm(torch.ones(512, dtype=torch.bfloat16))
+    assert lay.x.shape == (4, 512) and lay.x_codes.dtype == torch.uint8 and lay.rstd.numel() == 4
