@@ -86,14 +86,13 @@ __device__ __forceinline__ AdamStep step_numbers(const AdamArgs &a, const moe_ad
 // New m, v, sqrt(v) and parameter of one element.  The states' operations round one by one (no contraction, the correctly
 // rounded square root): where a state is held in codes, the last bit of a value can decide which code it gets, and this way the
 // codes are those of the formulas evaluated in fp32 by anyone.
-template <bool EIGHT>
 __device__ __forceinline__ void adam_element(const AdamStep &s, float g, float &p, float &m, float &v, float &root) {
   {
 #pragma clang fp contract(off)
     g = g * s.grad_scale;
     m = s.beta1 * m + s.new1 * g;
     v = s.beta2 * v + s.new2 * g * g;
-    root = EIGHT ? sqrtf(v) : __builtin_amdgcn_sqrtf(v);
+    root = sqrtf(v);  // (the instruction alone takes a subnormal v for 0, and eps may be less than its root)
   }
   p = fmaf(p, s.keep, -s.rate * m * __builtin_amdgcn_rcpf(fmaf(root, s.root2, s.eps)));
 }
@@ -228,7 +227,7 @@ struct AdamQuad {
         fv[q] = __uint_as_float(v[q]);
       }
       float fp = p[q];
-      adam_element<EIGHT>(s, grad(q), fp, fm[q], fv[q], root[q]);
+      adam_element(s, grad(q), fp, fm[q], fv[q], root[q]);
       p[q] = fp;
     }
     if constexpr (!EIGHT) {
@@ -292,8 +291,8 @@ struct AdamQuad {
 
 // PER blocks of 256 values for a wave, one behind the other; all are requested before the first is worked on.  32-bit
 // states: two.  8-bit states, whose blocks take 350 vector instructions each: four where a launch has the values to fill the chip
-// with that, else one (bf16 gradients and copies, 2^18 / 2^20 / 2^22 / 2^24 / 2^25 values: one block 3.7, 6.6, 16.7, 53.1 and 100.8 us,
-// four 6.4, 8.1, 17.6, 50.2 and 92.0).
+// with that, else one (bf16 gradients and copies, 2^18 / 2^20 / 2^22 / 2^23 / 2^24 / 2^25 values: one block 3.5, 5.8, 15.8, 26.7, 51.5
+// and 97.9 us, four 5.8, 7.8, 16.8, 27.2, 48.3 and 89.1).
 constexpr int kAdamFew = 1 << 22;
 constexpr int64_t adam_chunk_values(int per) { return (int64_t)per * kAdamThreads * 4; }
 template <bool EIGHT, bool BF16, int PER>

@@ -180,7 +180,7 @@ struct NormBackArgs {
 };
 
 // The weight's gradient of few rows, straight from the rows (it needs nothing of dx): a workgroup has sixteen pieces of columns, its
-// threads take 32 rows at a time, and the 32 sums of a column are added in order.
+// threads take 32 rows at a time (64 in workgroups of sixteen waves), and the sums of a column are added in order.
 constexpr int kNormColumns = 16;  // pieces
 template <typename T, int THREADS>
 __device__ __forceinline__ void norm_weight_grad_columns(const NormBackArgs &a, int block, float *dweight) {

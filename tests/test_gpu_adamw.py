@@ -220,6 +220,23 @@ def test_states_in_8_bits_keep_moving():
     assert start - mean > 0.5 * (start - free)  # and it has moved
 
 
+def test_small_gradients_with_a_small_eps():
+    """Gradients whose second state is subnormal in fp32 (below 1.2e-38), and zeros: a fresh state's first step is -lr g / (|g| + eps),
+    which for these is lr away from 0.  Tolerance: v = (1 - b2) g^2 is off by half a subnormal step, 2^-150, its root by half of that relative to
+    v (below 2e-3: 1 % for what is left out of the series); else the 32 u of an update."""
+    n, lr, eps = 4096, 1e-3, 1e-30
+    grad = 10 ** (torch.rand(n, generator=torch.Generator().manual_seed(5), dtype=torch.float64) * 4.7 - 19.7)
+    grad = (grad * (1 - 2 * (torch.arange(n) % 2))).float()
+    grad[::7] = 0
+    grad = grad.cuda()
+    p = torch.zeros(n, device="cuda")
+    L.AdamW([p], [grad], lr, 0.9, 0.999, eps).step()
+    g = grad.double()
+    off = 2.0 ** -150 / (1e-3 * g * g).clamp(min=1e-43) / 2 * 1.01 + 32 * U
+    assert ((p.double() + lr * g / (g.abs() + eps)).abs() <= lr * off).all()
+    assert (p[::7] == 0).all()
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_skipped_step_changes_nothing(bits):
     sizes = [5000, 33]
