@@ -512,7 +512,7 @@ typedef struct {
   uint32_t seed;
 } moe_adamw_device;
 typedef struct {
-  double beta1, beta2, eps; /* 0 <= beta < 1, eps > 0 */
+  double beta1, beta2, eps; /* 0 <= beta < 1, eps >= 2^-126 */
   int32_t state_bits;       /* 32 or 8 */
   moe_adamw_device now;
 } moe_adamw_config;

@@ -360,8 +360,8 @@ extern "C" int moe_adamw_step(const moe_adamw_config *config, const moe_adamw_te
                               const moe_adamw_device *device, void *stream) {
   if (!config || count < 0 || (count > 0 && !tensors)) return MOE_ERR_INVALID_ARG;
   const moe_adamw_config &c = *config;
-  if (!(c.beta1 >= 0 && c.beta1 < 1) || !(c.beta2 >= 0 && c.beta2 < 1) || !((float)c.eps > 0.f && c.eps < INFINITY))
-    return MOE_ERR_INVALID_ARG;
+  if (!(c.beta1 >= 0 && c.beta1 < 1) || !(c.beta2 >= 0 && c.beta2 < 1) || !((float)c.eps >= 0x1p-126f && c.eps < INFINITY))
+    return MOE_ERR_INVALID_ARG;  // (the reciprocal of a subnormal eps leaves fp32, and a state of zeros would give 0 times infinity)
   if (c.state_bits != 32 && c.state_bits != 8) return MOE_ERR_UNSUPPORTED;
   if (!device && (!(c.now.lr >= 0.f && c.now.lr < INFINITY) || c.now.step < 1)) return MOE_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(device) % 4 != 0) return MOE_ERR_INVALID_ARG;

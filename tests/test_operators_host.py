@@ -101,6 +101,11 @@ def test_adamw_refusals():
         assert adamw({"n": 4, **bad}, bits=8) == INV, bad
 
 
+def test_adamw_eps_is_a_normal_number():
+    assert adamw(eps=1e-39) == INV and adamw(eps=2.0 ** -127) == INV  # (their reciprocals leave fp32: 0 / eps would be NaN)
+    assert adamw(eps=2.0 ** -126) == 0 and adamw(eps=1e-30) == 0
+
+
 def test_adamw_class_checks_its_tensors():
     import torch
 
