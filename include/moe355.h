@@ -441,8 +441,9 @@ MOE355_API int moe_route_backward(const moe_shape *shape, const int32_t *topk_id
  *   s = x + residual, rounded to the element type (residual NULL: s = x), written to `sum` if that is not NULL;
  *   rstd = (mean over the row of s^2 + eps)^(-1/2) in fp32, written to rstd [rows] if that is not NULL;
  *   y = s rstd weight, formed in fp32 and rounded once, written if y is not NULL;
- *   codes [rows, cols], scales [rows] (both or neither): scale = largest magnitude of the row's y / 448 (1 for a zero row),
- *   code = cvt(y / scale), of y before its rounding to the element type.
+ *   codes [rows, cols], scales [rows] (both or neither): scale = largest magnitude of the row's y / 448 (1 for a zero row, and
+ *   2^-126 at least), code = cvt(y / scale), of y before its rounding to the element type; both are divisions in fp32, rounded
+ *   correctly, as in moe_fp8_quantize_rows.
  * At least one of y and codes is given; `sum` only with a residual, and it may be x or residual itself; y must be none of the
  * other arrays.  eps > 0.  Pointers 16-byte aligned (codes 8, scales and rstd 4).  A row with a NaN, an infinity or values whose
  * squares leave the range of fp32 (magnitudes of about 1e19) has no defined y, and a scale that is not finite where y is not.

@@ -113,6 +113,13 @@ namespace moe355 {
 
 __device__ __forceinline__ int lane_id() { return threadIdx.x & 63; }
 
+// a / b, correctly rounded, from b's correctly rounded reciprocal (Markstein 1990: with rcp = RN(1 / b) and q = RN(a rcp),
+// RN(q + RN(a - q b) rcp) is RN(a / b)), where a - q b is a normal number or exact.
+__device__ __forceinline__ float quotient(float a, float b, float rcp) {
+  const float q = a * rcp;
+  return __builtin_copysignf(fmaf(fmaf(-q, b, a), rcp, q), a);  // (the sum would lose the sign of a zero)
+}
+
 // Inclusive scan over the 64 lanes of a wave.
 __device__ __forceinline__ int wave_inclusive_scan(int v) {
   const int lane = lane_id();

@@ -23,13 +23,11 @@ __device__ __forceinline__ float amax_of(uint4 v, float m) {
   }
   return m;
 }
-// v / scale, correctly rounded, from the row's correctly rounded reciprocal (Markstein 1990: with rcp = RN(1 / b) and
-// q = RN(a rcp), RN(q + RN(a - q b) rcp) is RN(a / b)); the division itself costs a dozen instructions per element, half
+// v / scale, correctly rounded, from the row's reciprocal; the division itself costs a dozen instructions per element, half
 // the kernel's time on [4096, 7168].  Rows so small that an intermediate could leave the normal range divide (rcp = 0).
 __device__ __forceinline__ float divide_by(float a, float scale, float rcp) {
   if (rcp == 0.f) return a / scale;  // (the same in the whole workgroup)
-  const float q = a * rcp;
-  return __builtin_copysignf(fmaf(fmaf(-q, scale, a), rcp, q), a);  // (the sum would lose the sign of a zero)
+  return quotient(a, scale, rcp);
 }
 __device__ __forceinline__ uint2 codes_of(uint4 v, float scale, float rcp) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};

@@ -140,10 +140,13 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_kernel(
     for (int q = 0; q < N; ++q) top = MaxU()(top, __float_as_uint(v[i].get(q) * rstd * w[i].get(q)) & 0x7FFFFFFFu);
   top = row_reduce<WAVES>(top, tops, MaxU());
   const float amax = __uint_as_float(top);
-  // (2^-120: the reciprocal of a scale below is no normal number)
-  const float scale = top == 0u ? 1.0f : !(amax / 448.0f < 0x1p-120f) ? amax / 448.0f : 0x1p-120f;
-  const float inv = 1.0f / scale;
+  const float scale = top == 0u ? 1.0f : !(amax / 448.0f < 0x1p-126f) ? amax / 448.0f : 0x1p-126f;
   if (t == 0) a.scales[row] = scale;
+  // The quotients by the scale are rounded correctly: with bf16 inputs y / scale = 448 v w / (v w of the largest), of which four in
+  // 10^4 lie midway between two codes, and the last bit decides.  Both sides times 2^40 in rows of tiny values: the remainder of a
+  // quotient that is not code 0 (2^-10 and more, 24 bits of it, times 24 of the scale) then stays above 2^-149.
+  const float up = scale < 0x1p-80f ? 0x1p40f : 1.0f, divisor = scale * up;
+  const float inv = 1.0f / divisor;
 #pragma unroll
   for (int i = 0; i < CHUNKS; ++i) {
     const int c = t * N + i * STRIDE;
@@ -153,7 +156,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_kernel(
       float q[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        q[j] = __builtin_amdgcn_fmed3f(v[i].get(4 * g + j) * rstd * w[i].get(4 * g + j) * inv, 448.0f, -448.0f);
+        q[j] = __builtin_amdgcn_fmed3f(quotient(v[i].get(4 * g + j) * rstd * w[i].get(4 * g + j) * up, divisor, inv), 448.0f, -448.0f);
       int code = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
       packed[g] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], code, true);
     }
