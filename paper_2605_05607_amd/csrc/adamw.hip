@@ -84,8 +84,8 @@ __device__ __forceinline__ AdamStep step_numbers(const AdamArgs &a, const moe_ad
 }
 
 // New m, v, sqrt(v) and parameter of one element.  The states' operations round one by one (no contraction, the correctly
-// rounded square root): where a state is held in codes, the last bit of a value can decide which code it gets, and this way the
-// codes are those of the formulas evaluated in fp32 by anyone.
+// rounded square root), as do the scales (block_scale) and the quotients by them: where a state is held in codes, the last bit of a
+// value can decide which code it gets, and this way the codes are those of the formulas evaluated in fp32 by anyone.
 __device__ __forceinline__ void adam_element(const AdamStep &s, float g, float &p, float &m, float &v, float &root) {
   {
 #pragma clang fp contract(off)
@@ -99,10 +99,12 @@ __device__ __forceinline__ void adam_element(const AdamStep &s, float g, float &
 
 // E4M3 code of the magnitude of value / scale, rounded up where what is cut off exceeds the random bits (16, at the top of the 20 that
 // are cut).  Times 2^-120, the formats' exponent fields agree and E4M3's subnormal values are fp32's, so the code is the top of the
-// bit pattern throughout.  The quotient is the correctly rounded one, from the correctly rounded reciprocal (Markstein 1990).
+// bit pattern throughout.  The quotient is the correctly rounded one, but where the remainder falls under fp32's range (blocks whose
+// largest magnitude is below 2^-85) or the reciprocal is not (at most 33 of the 2^23 mantissas of a scale: all of them tried, with an
+// instruction's estimate one step off to either side); there it may be an ulp off.
 __device__ __forceinline__ uint32_t e4m3_stochastic(float v, float scale, float inv, uint32_t bits16) {
   const float a = fabsf(v), q0 = a * inv;
-  const float q = fmaf(fmaf(-q0, scale, a), inv, q0);
+  const float q = fmaf(fmaf(-q0, scale, a), inv, q0);  // (as quotient(), without the sign)
   return (__float_as_uint(fminf(q * 0x1p-120f, 448.0f * 0x1p-120f)) + (bits16 << 4)) >> 20;
 }
 
@@ -133,11 +135,12 @@ struct BlockScale {
   float scale, inv;
 };
 // The scale of the 256 values of a wave, from the largest bit pattern of their magnitudes (a NaN or an infinity gives a scale
-// of NaN, so that the block shows it).  Below 2^-100 a block counts as zero: the reciprocal of its scale is no normal number.
+// of NaN, so that the block shows it): largest / 448, correctly rounded.  Below 2^-100 a block counts as zero: the reciprocal of its
+// scale is no normal number.  (Square roots of numbers in fp32 are 2^-75 and more, or 0.)
 __device__ __forceinline__ BlockScale block_scale(uint32_t top) {
   top = wave_max(top);
   const bool finite = top < 0x7F800000u, some = top >= 0x0D800000u;
-  const float scale = some ? __uint_as_float(top) * (1.0f / 448.0f) : 1.0f;
+  const float scale = some ? quotient(__uint_as_float(top), 448.0f, 1.0f / 448.0f) : 1.0f;
   const float r = __builtin_amdgcn_rcpf(scale);
   return {finite ? scale : __builtin_nanf(""), finite && some ? fmaf(fmaf(-scale, r, 1.0f), r, r) : 0.0f};
 }

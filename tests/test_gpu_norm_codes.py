@@ -36,5 +36,5 @@ def test_codes_are_those_of_the_divisions(rows, cols, dtype):
             B.moe_rmsnorm(rows, cols, code, x, None, w.to(dt), eps, None, None, q, sc, rstd)
             want, scales = codes_of(x, rstd, w.to(dt))
             off = (q.cpu() != want).sum(1)
-            assert int(off[:: len(size)].sum()) == 0 and int(off.sum()) == 0  # rows of size 1; all
-            assert int((sc.cpu() != scales).sum()) == 0
+            plain, every, of_scales = int(off[:: len(size)].sum()), int(off.sum()), int((sc.cpu() != scales).sum())
+            assert plain == 0 and every == 0 and of_scales == 0  # (plain: rows of size 1)
