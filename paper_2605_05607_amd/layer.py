@@ -41,6 +41,8 @@ class MoELayer:
         self.y = torch.empty((max(1, s.T), s.d), dtype=self.elt_dtype, device=device)
         self.packed_gate_up = None
         self.packed_down = None
+        self.fp8_gate_up = None
+        self.fp8_down = None
 
     def load_weights(self, W_gate: np.ndarray, W_up: np.ndarray, W_down: np.ndarray) -> None:
         import torch
@@ -135,10 +137,14 @@ class MoELayer:
         self.optimizer = AdamW(self.masters, [self.dW_gate, self.dW_up, self.dW_down], lr, copies=self.weights, **kw)
 
     def optimizer_step(self, **kw) -> None:
-        """The step with the gradients of the last `backward`, and the new weights packed for the next forward and backward."""
+        """The step with the gradients of the last `backward`, and the new weights packed for the next forward and backward, in every
+        form that the layer holds (FP8 too after load_weights_fp8; h_scale stays as it is).  A captured step packs the forms that
+        were there when it was captured."""
         self.optimizer.step(**kw)
         B.moe_pack_weights(self.shape, *self.weights, self.packed_gate_up, self.packed_down)
         B.moe_pack_weights_backward(self.shape, *self.weights, self.packed_down_t, self.packed_gate_up_t)
+        if self.fp8_gate_up is not None:
+            B.moe_fp8_pack_weights(self.shape, *self.weights, self.fp8_gate_up, self.fp8_down)
 
     def forward_train(self, x) -> None:
         B.moe_fused_forward_train(self.shape, x, self.topk_idx, self.topk_w, self.tables, self.packed_gate_up,
