@@ -43,6 +43,7 @@ class MoELayer:
         self.packed_down = None
         self.fp8_gate_up = None
         self.fp8_down = None
+        self.optimizer = None
 
     def load_weights(self, W_gate: np.ndarray, W_up: np.ndarray, W_down: np.ndarray) -> None:
         import torch
@@ -127,11 +128,11 @@ class MoELayer:
             self.dW_gate = self.dW_up = self.dW_down = None
 
     def enable_optimizer(self, W_gate: np.ndarray, W_up: np.ndarray, W_down: np.ndarray, lr: float, **kw) -> None:
-        """An AdamW step on the three expert weights, after enable_training with weight gradients: fp32 parameters, bf16 copies of
-        them and the optimizer (`kw` as for AdamW)."""
+        """An AdamW step on the three expert weights, after load_weights and enable_training with weight gradients: fp32 parameters,
+        bf16 copies of them and the optimizer (`kw` as for AdamW)."""
         import torch
-        if getattr(self, "dW_gate", None) is None:
-            raise ValueError("enable_training with weight gradients comes first")
+        if getattr(self, "dW_gate", None) is None or self.packed_gate_up is None:
+            raise ValueError("load_weights and enable_training with weight gradients come first")
         self.weights = [to_device(a, self.device) for a in (W_gate, W_up, W_down)]
         self.masters = [w.to(torch.float32) for w in self.weights]
         self.optimizer = AdamW(self.masters, [self.dW_gate, self.dW_up, self.dW_down], lr, copies=self.weights, **kw)
@@ -140,6 +141,8 @@ class MoELayer:
         """The step with the gradients of the last `backward`, and the new weights packed for the next forward and backward, in every
         form that the layer holds (FP8 too after load_weights_fp8; h_scale stays as it is).  A captured step packs the forms that
         were there when it was captured."""
+        if self.optimizer is None:
+            raise ValueError("enable_optimizer comes first")
         self.optimizer.step(**kw)
         B.moe_pack_weights(self.shape, *self.weights, self.packed_gate_up, self.packed_down)
         B.moe_pack_weights_backward(self.shape, *self.weights, self.packed_down_t, self.packed_gate_up_t)

@@ -1,0 +1,37 @@
+"""What the optimizers refuse, and what a refused or skipped call leaves, without a GPU."""
+import pytest
+import torch
+
+from paper_2605_05607_amd import binding as B
+from paper_2605_05607_amd import layer as L
+from paper_2605_05607_amd import workloads as wl
+
+
+@pytest.fixture
+def packs(monkeypatch):
+    """The library's calls that a layer on the CPU cannot make, by name."""
+    calls = []
+    for name in ("moe_pack_weights", "moe_pack_weights_backward", "moe_adamw_step"):
+        monkeypatch.setattr(B, name, lambda *a, _n=name, **k: calls.append(_n))
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda: None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: None)
+    return calls
+
+
+def layer_and_weights():
+    cfg = wl.CONFIGS["tiny"].scaled(T=4, dtype=wl.BF16)
+    w = wl.make_workload(cfg)
+    return L.MoELayer(cfg, device="cpu"), (w.W_gate, w.W_up, w.W_down)
+
+
+def test_optimizer_asks_for_both_packings(packs):
+    lay, w = layer_and_weights()
+    lay.enable_training(*w)
+    with pytest.raises(ValueError):  # no forward weights to pack a step into
+        lay.enable_optimizer(*w, 1e-3)
+    with pytest.raises(ValueError):
+        lay.optimizer_step()
+    lay.load_weights(*w)
+    lay.enable_optimizer(*w, 1e-3)
+    lay.optimizer_step()
+    assert packs[-3:] == ["moe_adamw_step", "moe_pack_weights", "moe_pack_weights_backward"]
