@@ -50,6 +50,7 @@ class MoELayer:
         s = self.shape
         self.packed_gate_up = torch.empty(B.moe_packed_weight_bytes(s, 0), dtype=torch.uint8, device=self.device)
         self.packed_down = torch.empty(B.moe_packed_weight_bytes(s, 1), dtype=torch.uint8, device=self.device)
+        self.optimizer = None  # (it has weights of its own, and would bring those back)
         g, u, d = (to_device(a, self.device) for a in (W_gate, W_up, W_down))
         B.moe_pack_weights(s, g, u, d, self.packed_gate_up, self.packed_down)
         torch.cuda.synchronize()
@@ -109,6 +110,7 @@ class MoELayer:
         import torch
         s = self.shape
         dev = self.device
+        self.optimizer = None  # (it has the present weights, and reads the present gradients)
         self.packed_down_t = torch.empty(B.moe_backward_packed_weight_bytes(s, 0), dtype=torch.uint8, device=dev)
         self.packed_gate_up_t = torch.empty(B.moe_backward_packed_weight_bytes(s, 1), dtype=torch.uint8, device=dev)
         g, u, d = (to_device(a, dev) for a in (W_gate, W_up, W_down))
@@ -129,7 +131,7 @@ class MoELayer:
 
     def enable_optimizer(self, W_gate: np.ndarray, W_up: np.ndarray, W_down: np.ndarray, lr: float, **kw) -> None:
         """An AdamW step on the three expert weights, after load_weights and enable_training with weight gradients: fp32 parameters,
-        bf16 copies of them and the optimizer (`kw` as for AdamW)."""
+        bf16 copies of them and the optimizer (`kw` as for AdamW).  Either of the two called again ends it."""
         import torch
         if getattr(self, "dW_gate", None) is None or self.packed_gate_up is None:
             raise ValueError("load_weights and enable_training with weight gradients come first")
@@ -142,7 +144,7 @@ class MoELayer:
         form that the layer holds (FP8 too after load_weights_fp8; h_scale stays as it is).  A captured step packs the forms that
         were there when it was captured."""
         if self.optimizer is None:
-            raise ValueError("enable_optimizer comes first")
+            raise ValueError("enable_optimizer comes first, and again after load_weights or enable_training")
         self.optimizer.step(**kw)
         B.moe_pack_weights(self.shape, *self.weights, self.packed_gate_up, self.packed_down)
         B.moe_pack_weights_backward(self.shape, *self.weights, self.packed_down_t, self.packed_gate_up_t)

@@ -35,3 +35,21 @@ def test_optimizer_asks_for_both_packings(packs):
     lay.enable_optimizer(*w, 1e-3)
     lay.optimizer_step()
     assert packs[-3:] == ["moe_adamw_step", "moe_pack_weights", "moe_pack_weights_backward"]
+
+
+def test_optimizer_ends_with_the_weights_and_gradients_that_it_was_made_for(packs):
+    """Other weights, or other buffers for the gradients: a step would bring the old weights back, or read gradients that no backward
+    pass writes any more."""
+    for other in ("load_weights", "enable_training"):
+        lay, w = layer_and_weights()
+        lay.load_weights(*w)
+        lay.enable_training(*w)
+        lay.enable_optimizer(*w, 1e-3)
+        getattr(lay, other)(*w)
+        packs.clear()
+        with pytest.raises(ValueError):
+            lay.optimizer_step()
+        assert not packs
+        lay.enable_optimizer(*w, 1e-3)
+        lay.optimizer_step()
+        assert "moe_adamw_step" in packs
