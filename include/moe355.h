@@ -488,7 +488,7 @@ MOE355_API int moe_dispatch_gather_backward(const moe_shape *shape, const void *
 /*
  * One AdamW step over a list of tensors (the weights of a layer, with the gradients of moe_fused_backward), in place:
  *   g = grad_scale grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
- *   param = param (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps),
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps),
  *   copy = param rounded to bf16 (where copy is not NULL).
  * The list is read by the host during the call; the arrays are device memory.  param fp32 [n], copy bf16 [n], grad [n] in
  * grad_dtype, all 16-byte aligned; n = 0 is an empty tensor.  No array may be part of two tensors of one call.
@@ -498,12 +498,13 @@ MOE355_API int moe_dispatch_gather_backward(const moe_shape *shape, const void *
  *     below 2^-100 counts as one; a fresh state is codes 0).  The step is taken with the new m and v before they are rounded.  A
  *     code is rounded up with the probability of the part that is cut off, from 16 bits of a hash: with mix(z): z = (z ^ z >> 16) * 0x6A09E667, z = (z ^ z >> 15) * 0xBB67AE85,
  *     z ^ z >> 16 (mod 2^32), element i of tensor k of the list has h = mix(low word of i ^ mix(high word of i + mix(seed +
- *     mix(step + mix(k + 0x9E3779B9))))), m its low and sqrt(v) its high half.  A positive sqrt(v) never gets code 0.
+ *     mix(t + mix(k + 0x9E3779B9))))), m its low and sqrt(v) its high half.  A positive sqrt(v) never gets code 0.
  *     A block that holds a value that is not finite gets the scale NaN.
- * The step's own numbers, moe_adamw_device: step counts from 1.  They come from config->now, or, where `device` is not NULL, from
- * that device memory when the kernels run (for captured steps: write it between replays; lr and step are then not checked).
- * A grad_scale that is not finite leaves every array as it was (a step whose gradients have overflowed is skipped without a
- * word from the host).  Same inputs, same bits; the states' fp32 operations are rounded one by one.
+ * The step's own numbers, moe_adamw_device, come from config->now, or, where `device` is not NULL, from that device memory when the
+ * kernels run (for captured steps: write it between replays; lr, step and skipped are then not checked).  A grad_scale that is not
+ * finite leaves every array as it was (a step whose gradients have overflowed is skipped without a word from the host).  step counts
+ * from 1, and t = step - skipped: the averages know nothing of skipped steps, and their correction must not count them.  Same inputs,
+ * same bits; the states' fp32 operations are rounded one by one.
  */
 #define MOE_ADAMW_BLOCK 256
 typedef struct {
@@ -511,6 +512,7 @@ typedef struct {
   float grad_scale;
   int32_t step;
   uint32_t seed;
+  int32_t skipped; /* of the steps so far, with this one: those that left everything as it was, 0 <= skipped < step */
 } moe_adamw_device;
 typedef struct {
   double beta1, beta2, eps; /* 0 <= beta < 1, eps >= 2^-126 */

@@ -33,7 +33,8 @@ class moe_dispatch(C.Structure):
 
 
 class moe_adamw_device(C.Structure):
-    _fields_ = [("lr", C.c_float), ("grad_scale", C.c_float), ("step", C.c_int32), ("seed", C.c_uint32)]
+    _fields_ = [("lr", C.c_float), ("grad_scale", C.c_float), ("step", C.c_int32), ("seed", C.c_uint32),
+                ("skipped", C.c_int32)]
 
 
 class moe_adamw_config(C.Structure):

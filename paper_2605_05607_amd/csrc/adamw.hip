@@ -77,8 +77,8 @@ __device__ __forceinline__ AdamStep step_numbers(const AdamArgs &a, const moe_ad
   s.new2 = a.new2;
   s.eps = a.eps;
   s.keep = 1.0f - now.lr * x.weight_decay;
-  s.rate = now.lr / one_less_power((float)now.step * a.log_beta1);
-  s.root2 = 1.0f / sqrtf(one_less_power((float)now.step * a.log_beta2));
+  s.rate = now.lr / one_less_power((float)(now.step - now.skipped) * a.log_beta1);
+  s.root2 = 1.0f / sqrtf(one_less_power((float)(now.step - now.skipped) * a.log_beta2));
   s.grad_scale = now.grad_scale;
   return s;
 }
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
       (int)__popcll(__ballot(lane + 1 < a.count && chunk >= a.first[min(lane + 1, kAdamTensors)])));
   const AdamTensor &x = a.tensor[k];
   const int64_t begin = (int64_t)(chunk - a.first[k]) * adam_chunk_values(PER);
-  const uint32_t key = EIGHT ? mix(now.seed + mix((uint32_t)now.step + mix((uint32_t)(a.index0 + k) + 0x9E3779B9u))) : 0u;
+  const uint32_t key = EIGHT ? mix(now.seed + mix((uint32_t)(now.step - now.skipped) + mix((uint32_t)(a.index0 + k) + 0x9E3779B9u))) : 0u;
   if (x.grad_bf16) adam_chunk<EIGHT, true, PER>(a, now, x, begin, key); else adam_chunk<EIGHT, false, PER>(a, now, x, begin, key);
 }
 
@@ -366,7 +366,8 @@ extern "C" int moe_adamw_step(const moe_adamw_config *config, const moe_adamw_te
   if (!(c.beta1 >= 0 && c.beta1 < 1) || !(c.beta2 >= 0 && c.beta2 < 1) || !((float)c.eps >= 0x1p-126f && c.eps < INFINITY))
     return MOE_ERR_INVALID_ARG;  // (the reciprocal of a subnormal eps leaves fp32, and a state of zeros would give 0 times infinity)
   if (c.state_bits != 32 && c.state_bits != 8) return MOE_ERR_UNSUPPORTED;
-  if (!device && (!(c.now.lr >= 0.f && c.now.lr < INFINITY) || c.now.step < 1)) return MOE_ERR_INVALID_ARG;
+  if (!device && (!(c.now.lr >= 0.f && c.now.lr < INFINITY) || c.now.skipped < 0 || c.now.step <= c.now.skipped))
+    return MOE_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(device) % 4 != 0) return MOE_ERR_INVALID_ARG;
   const bool eight = c.state_bits == 8;
   for (int k = 0; k < count; ++k) {

@@ -2,6 +2,8 @@
 to the library.  No arithmetic happens here."""
 from __future__ import annotations
 
+import math
+
 import numpy as np
 
 from . import binding as B
@@ -210,8 +212,9 @@ class AdamW:
     grads: a tensor for each parameter, fp32 or bf16, read by every step.  copies: None, or a bf16 tensor (or None) for each
     parameter that receives its rounded value.  bits: 32 or 8, the states' width (8: E4M3 codes of m and of sqrt(v), a scale per
     256 values).  weight_decay: one number, or one for each parameter.  states: [(m, v, m_scale, v_scale)] to go on from, zeros
-    without; steps: steps taken so far.  device_scalars: the step's number, lr and grad_scale live in device memory
-    (``scalars``), so that a captured ``step`` advances with every replay; change them there.
+    without; steps: steps taken so far, without skipped ones, as ``steps`` tells them.  device_scalars: lr, grad_scale and the
+    number of the call live in device memory (``scalars``), so that a captured ``step`` advances with every replay; change lr and
+    grad_scale there.
     """
 
     def __init__(self, params, grads, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, copies=None, bits=32, seed=0,
@@ -246,21 +249,30 @@ class AdamW:
         if len(set(written)) < len(written):
             raise ValueError("a tensor that a step writes is there twice")
         self.params, self.grads, self.copies, self.states = list(params), list(grads), copies, states
-        self.steps = steps
+        self._steps = steps
         self.config = B.moe_adamw_config(beta1, beta2, eps, bits, B.moe_adamw_device(lr, 1.0, 0, seed))
         self._list = (B.moe_adamw_tensor * max(1, n))(*[
             B.moe_adamw_tensor(*(B._ptr(t) for t in (p, c, g, *s)), p.numel(), d,
                                B.MOE_BF16 if g.dtype == torch.bfloat16 else B.MOE_F32)
             for p, g, c, s, d in zip(params, grads, copies, states, decay)])
-        self.scalars = self._count = None
-        if device_scalars and n:  # a moe_adamw_device: lr and grad_scale as floats, the step's number, the seed
-            words = np.array([lr, 1.0], dtype=np.float32).view(np.int32).tolist() + [steps, int(np.uint32(seed).view(np.int32))]
-            self.scalars = torch.tensor(words, dtype=torch.int32, device=params[0].device)
-            self._count = self.scalars[2:3]
+        self.scalars = None
+        if device_scalars and n:  # a moe_adamw_device: lr and grad_scale as floats, the call's number, the seed; the skipped calls
+            words = np.array([lr, 1.0], dtype=np.float32).view(np.int32).tolist() + [steps, int(np.uint32(seed).view(np.int32)), 0]
+            self._device = torch.tensor(words, dtype=torch.int32, device=params[0].device)
+            self.scalars, self._count, self._skipped = self._device[:4], self._device[2:3], self._device[4:]
+            self._scale = self._device.view(torch.float32)[1:2]
+
+    @property
+    def steps(self) -> int:
+        """Steps taken, without skipped ones.  With device scalars those of the device: waits for it."""
+        if self.scalars is None:
+            return self._steps
+        words = self._device.tolist()
+        return words[2] - words[4]
 
     def step(self, lr=None, grad_scale=1.0) -> None:
         """One step with the gradients as they are.  lr: a new rate from now on.  grad_scale: multiplies the gradients; one that is
-        not finite skips the step, which counts all the same.  With device scalars both are set there."""
+        not finite skips the step, which then does not count in the averages' corrections.  With device scalars both are set there."""
         if self.scalars is not None:
             if lr is not None or grad_scale != 1.0:
                 raise ValueError("lr and grad_scale are in `scalars`")
@@ -270,9 +282,11 @@ class AdamW:
                 return self.step(lr, grad_scale)
         if self.scalars is not None:
             self._count += 1
+            self._skipped += (self._scale - self._scale).ne(0)  # (0 where it is finite, else NaN)
         elif lr is not None:
             self.config.now.lr = lr
         self.config.now.grad_scale = grad_scale
-        self.config.now.step = self.steps + 1
+        self.config.now.step = self._steps + 1
         B.moe_adamw_step(self.config, self._list, len(self.params), self.scalars)
-        self.steps += 1
+        if self.scalars is None and math.isfinite(self.config.now.grad_scale):
+            self._steps += 1

@@ -1,4 +1,6 @@
 """What the optimizers refuse, and what a refused or skipped call leaves, without a GPU."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -53,3 +55,25 @@ def test_optimizer_ends_with_the_weights_and_gradients_that_it_was_made_for(pack
         lay.enable_optimizer(*w, 1e-3)
         lay.optimizer_step()
         assert "moe_adamw_step" in packs
+
+
+def test_skipped_steps_do_not_count(packs):
+    p, g = torch.zeros(10), torch.zeros(10)
+    opt = L.AdamW([p], [g], 1e-3, steps=4)
+    for scale, steps in ((1.0, 5), (float("inf"), 5), (float("nan"), 5), (0.5, 6), (1e39, 6)):  # (1e39 is infinite in fp32)
+        opt.step(grad_scale=scale)
+        assert opt.steps == steps
+    opt = L.AdamW([p], [g], 1e-3, steps=4, device_scalars=True)
+    words = opt.scalars.view(torch.float32)
+    for scale, steps in ((1.0, 5), (float("inf"), 5), (float("-inf"), 5), (float("nan"), 5), (0.5, 6)):
+        words[1] = scale
+        opt.step()
+        assert opt.steps == steps
+    assert opt.scalars.tolist()[2] == 9  # calls
+
+
+def test_numbers_of_steps_that_cannot_be():
+    t = B.moe_adamw_tensor(None, None, None, None, None, None, None, 0, 0.0, B.MOE_F32)
+    for step, skipped, ok in ((1, 0, True), (3, 2, True), (3, 3, False), (1, 1, False), (2, -1, False), (-2 ** 31, 2 ** 31 - 1, False)):
+        c = B.moe_adamw_config(0.9, 0.99, 1e-8, 32, B.moe_adamw_device(1e-3, 1.0, step, 0, skipped))
+        assert (B.lib().moe_adamw_step(C.byref(c), C.byref(t), 1, None, None) == B.MOE_OK) == ok, (step, skipped)
