@@ -87,6 +87,8 @@ class MoELayer:
         self.norm_weight = weight if isinstance(weight, torch.Tensor) else to_device(weight, dev)
         if self.norm_weight.dtype != self.elt_dtype or self.norm_weight.numel() != s.d:
             raise ValueError("the norm's weight has d values in the layer's element type")
+        if self.norm_weight.device != self.y.device or not self.norm_weight.is_contiguous():
+            raise ValueError("the norm's weight is contiguous, on the layer's device")
         self.norm_eps = eps
         self.norm_sum, self.x = (torch.empty((max(1, s.T), s.d), dtype=self.elt_dtype, device=dev) for _ in range(2))
         self.x_codes = torch.empty((max(1, s.T), s.d), dtype=torch.uint8, device=dev)

@@ -77,3 +77,13 @@ def test_numbers_of_steps_that_cannot_be():
     for step, skipped, ok in ((1, 0, True), (3, 2, True), (3, 3, False), (1, 1, False), (2, -1, False), (-2 ** 31, 2 ** 31 - 1, False)):
         c = B.moe_adamw_config(0.9, 0.99, 1e-8, 32, B.moe_adamw_device(1e-3, 1.0, step, 0, skipped))
         assert (B.lib().moe_adamw_step(C.byref(c), C.byref(t), 1, None, None) == B.MOE_OK) == ok, (step, skipped)
+
+
+def test_norm_weight_is_the_layer_s_own_kind_of_memory():
+    """The library is given its address: elsewhere or strided it would be read wrongly."""
+    lay, _ = layer_and_weights()
+    d = lay.shape.d
+    for w in (torch.ones(d, dtype=torch.bfloat16, device="meta"), torch.ones((d, 2), dtype=torch.bfloat16)[:, 0]):
+        with pytest.raises(ValueError):
+            lay.enable_norm(w)
+    lay.enable_norm(torch.ones(1, d, dtype=torch.bfloat16))
