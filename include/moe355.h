@@ -491,7 +491,7 @@ MOE355_API int moe_dispatch_gather_backward(const moe_shape *shape, const void *
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps),
  *   copy = param rounded to bf16 (where copy is not NULL).
  * The list is read by the host during the call; the arrays are device memory.  param fp32 [n], copy bf16 [n], grad [n] in
- * grad_dtype, all 16-byte aligned; n = 0 is an empty tensor.  No array may be part of two tensors of one call.
+ * grad_dtype, all 16-byte aligned; n = 0 is an empty tensor.  No array that is written may overlap another one of the call.
  *   state_bits 32: m, v fp32 [n], 16-byte aligned; the scales are not read.
  *   state_bits 8:  m, v uint8 [n], 16-byte aligned, m_scale, v_scale fp32 [ceil(n / MOE_ADAMW_BLOCK)]: E4M3 codes of m / scale and
  *     of sqrt(v) / scale, one scale per MOE_ADAMW_BLOCK values = largest magnitude / 448 (1 for a block of zeros, and a block of m

@@ -212,11 +212,11 @@ class AdamW:
     """One optimizer over a list of fp32 device tensors: holds both states and forwards every step to moe_adamw_step.
 
     grads: a tensor for each parameter, fp32 or bf16, read by every step.  copies: None, or a bf16 tensor (or None) for each
-    parameter that receives its rounded value.  bits: 32 or 8, the states' width (8: E4M3 codes of m and of sqrt(v), a scale per
-    256 values).  weight_decay: one number, or one for each parameter.  states: [(m, v, m_scale, v_scale)] to go on from, zeros
-    without; steps: steps taken so far, without skipped ones, as ``steps`` tells them.  device_scalars: lr, grad_scale and the
-    number of the call live in device memory (``scalars``), so that a captured ``step`` advances with every replay; change lr and
-    grad_scale there.
+    parameter that receives its rounded value.  All arrays stay where they are in memory.  bits: 32 or 8, the states' width (8:
+    E4M3 codes of m and of sqrt(v), a scale per 256 values).  weight_decay: one number, or one for each parameter.  states:
+    [(m, v, m_scale, v_scale)] to go on from, zeros without; steps: steps taken so far, without skipped ones, as ``steps`` tells
+    them.  device_scalars: lr, grad_scale and the number of the call live in device memory (``scalars``), so that a captured
+    ``step`` advances with every replay; change lr and grad_scale there.  (Captured without, every replay is the same step.)
     """
 
     def __init__(self, params, grads, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, copies=None, bits=32, seed=0,
@@ -247,9 +247,14 @@ class AdamW:
             for t, dtype, size in held:
                 if t is None or t.dtype != dtype or t.numel() != size or not t.is_contiguous() or t.device != params[0].device:
                     raise ValueError("contiguous tensors of the parameter's size on one device: fp32 parameters, bf16 copies")
-        written = [t.data_ptr() for t in (*params, *copies, *(t for s in states for t in s)) if t is not None and t.numel()]
-        if len(set(written)) < len(written):
-            raise ValueError("a tensor that a step writes is there twice")
+        held = [(t, True) for t in (*params, *copies, *(t for s in states for t in s[: 4 if bits == 8 else 2]))]
+        held = [(t, w) for t, w in held + [(g, False) for g in grads] if t is not None and t.numel()]
+        end = end_written = 0  # of the arrays that begin before this one
+        for at, size, w in sorted((t.data_ptr(), t.numel() * t.element_size(), w) for t, w in held):
+            if at < (end if w else end_written):
+                raise ValueError("an array that a step writes overlaps another one")
+            end = max(end, at + size)
+            end_written = max(end_written, at + size) if w else end_written
         self.params, self.grads, self.copies, self.states = list(params), list(grads), copies, states
         self._steps = steps
         self.config = B.moe_adamw_config(beta1, beta2, eps, bits, B.moe_adamw_device(lr, 1.0, 0, seed))

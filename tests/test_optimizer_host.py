@@ -87,3 +87,18 @@ def test_norm_weight_is_the_layer_s_own_kind_of_memory():
         with pytest.raises(ValueError):
             lay.enable_norm(w)
     lay.enable_norm(torch.ones(1, d, dtype=torch.bfloat16))
+
+
+def test_arrays_of_an_optimizer_do_not_overlap():
+    flat, g = torch.zeros(100), torch.zeros(60)
+    for p in ([flat[:60], flat[40:]], [flat[40:], flat[:60]], [flat, flat[20:80]]):
+        with pytest.raises(ValueError):
+            L.AdamW(p, [torch.zeros(t.numel()) for t in p], 1e-3)
+    halves = [flat[:50], flat[50:]]
+    with pytest.raises(ValueError):  # a gradient that the step of another tensor writes
+        L.AdamW(halves, [flat[50:], torch.zeros(50)], 1e-3)
+    L.AdamW(halves, [g[:50], g[:50]], 1e-3)  # (one gradient for both is only read)
+    L.AdamW([flat[:0], flat[50:50], flat], [g[:0], g[:0], flat + 0], 1e-3)
+    state = torch.zeros(100)
+    with pytest.raises(ValueError):
+        L.AdamW(halves, [g[:50], g[:50]], 1e-3, states=[(state[:50], state[50:], None, None), (state[25:75], flat + 0, None, None)])
