@@ -290,10 +290,14 @@ class AdamW:
         if self.scalars is not None:
             self._count += 1
             self._skipped += (self._scale - self._scale).ne(0)  # (0 where it is finite, else NaN)
-        elif lr is not None:
-            self.config.now.lr = lr
-        self.config.now.grad_scale = grad_scale
-        self.config.now.step = self._steps + 1
-        B.moe_adamw_step(self.config, self._list, len(self.params), self.scalars)
-        if self.scalars is None and math.isfinite(self.config.now.grad_scale):
+        now = self.config.now
+        held, now.lr = now.lr, now.lr if lr is None else lr
+        now.grad_scale = grad_scale
+        now.step = self._steps + 1
+        try:
+            B.moe_adamw_step(self.config, self._list, len(self.params), self.scalars)
+        except B.MoeError:
+            now.lr = held
+            raise
+        if self.scalars is None and math.isfinite(now.grad_scale):
             self._steps += 1

@@ -102,3 +102,17 @@ def test_arrays_of_an_optimizer_do_not_overlap():
     state = torch.zeros(100)
     with pytest.raises(ValueError):
         L.AdamW(halves, [g[:50], g[:50]], 1e-3, states=[(state[:50], state[50:], None, None), (state[25:75], flat + 0, None, None)])
+
+
+def test_refused_step_leaves_the_rate(packs, monkeypatch):
+    p, g = torch.zeros(10), torch.zeros(10)
+    opt = L.AdamW([p], [g], 1e-3)
+
+    def refuse(*a, **k):
+        raise B.MoeError(B.MOE_ERR_INVALID_ARG, "moe_adamw_step")
+    with monkeypatch.context() as m:
+        m.setattr(B, "moe_adamw_step", refuse)
+        with pytest.raises(B.MoeError):
+            opt.step(lr=-1.0)
+    opt.step()
+    assert opt.steps == 1 and abs(opt.config.now.lr - 1e-3) < 1e-9
