@@ -444,16 +444,17 @@ MOE355_API int moe_route_backward(const moe_shape *shape, const int32_t *topk_id
  *   codes [rows, cols], scales [rows] (both or neither): scale = largest magnitude of the row's y / 448 (1 for a zero row, and
  *   2^-126 at least), code = cvt(y / scale), of y before its rounding to the element type; both are divisions in fp32, rounded
  *   correctly, as in moe_fp8_quantize_rows.
- * At least one of y and codes is given; `sum` only with a residual, and it may be x or residual itself; y must be none of the
- * other arrays.  eps > 0.  Pointers 16-byte aligned (codes 8, scales and rstd 4).  A row with a NaN, an infinity or values whose
- * squares leave the range of fp32 (magnitudes of about 1e19) has no defined y, and a scale that is not finite where y is not.
+ * At least one of y and codes is given; `sum` only with a residual, and it may be x or residual itself; else no array that is
+ * written may overlap another one.  eps > 0.  Pointers 16-byte aligned (codes 8, scales and rstd 4).  A row with a NaN, an
+ * infinity or values whose squares leave the range of fp32 (magnitudes of about 1e19) has no defined y, and a scale that is not
+ * finite where y is not.
  *
  * moe_rmsnorm_backward: with a = dy weight,
  *   dx = rstd (a - s rstd^2 mean(a s)) + dsum,   dweight[c] = sum over the rows of dy s rstd.
  *   sum: s as the forward wrote it (without a residual: x); rstd as the forward wrote it; dy [rows, cols]; dsum [rows, cols] the
  *   gradient that reaches s directly, down the residual stream (NULL: none); dx [rows, cols] the gradient of x and of the
- *   residual alike, it may be dy or dsum itself; dweight [cols] fp32 (NULL: not wanted, and no workspace needed), written in
- *   full.  Sums in fp32 in an order that depends on the sizes only (dweight's of up to 512 rows also on whether dx is dy): same
+ *   residual alike, it may be dy or dsum itself (else, what is written overlaps no other array); dweight [cols] fp32 (NULL: not
+ *   wanted, and no workspace needed), written in full.  Sums in fp32 in an order that depends on the sizes only (dweight's of up to 512 rows also on whether dx is dy): same
  *   inputs, same bits.  workspace >=
  *   moe_rmsnorm_backward_workspace_bytes(rows, cols) (0 for invalid sizes), 16-byte aligned; a buffer for more rows serves fewer.
  */

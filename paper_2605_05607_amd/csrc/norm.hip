@@ -7,6 +7,7 @@
 // Bound by HBM: a handful of fp32 operations per element read.  A row stays in the registers of its threads from its one read
 // to its writes; statistics and all sums are fp32, and what is stored in the element type is rounded once.
 #include <algorithm>
+#include <initializer_list>
 
 #include "forward_types.h"
 
@@ -496,6 +497,21 @@ static int norm_backward(NormBackArgs a, float *dweight, hipStream_t st) {
 static bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 static bool aligned4(const void *p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
+// An array of a call (p null: not there).
+struct Extent {
+  const void *p;
+  size_t bytes;
+};
+// Does `a` share memory with one of the others?
+static bool overlaps(const Extent &a, std::initializer_list<Extent> others) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(a.p);
+  for (const Extent &b : others) {
+    const uintptr_t with = reinterpret_cast<uintptr_t>(b.p);
+    if (a.p && b.p && a.bytes && b.bytes && at < with + b.bytes && with < at + a.bytes) return true;
+  }
+  return false;
+}
+
 }  // namespace moe355
 
 using namespace moe355;
@@ -510,6 +526,12 @@ extern "C" int moe_rmsnorm(int64_t rows, int cols, int dtype, const void *x, con
       reinterpret_cast<uintptr_t>(codes) % 8 != 0 || !aligned4(scales) || !aligned4(rstd))
     return MOE_ERR_INVALID_ARG;
   if (y && (y == x || y == residual || y == sum || y == codes)) return MOE_ERR_INVALID_ARG;
+  const size_t cells = (size_t)rows * cols, elt = dtype == MOE_BF16 ? 2 : 4;
+  const Extent in{x, cells * elt}, res{residual, cells * elt}, w{weight, cols * elt}, s{sum, cells * elt}, out{y, cells * elt},
+      q{codes, cells}, sc{scales, rows * sizeof(float)}, r{rstd, rows * sizeof(float)};
+  if (overlaps(out, {in, res, w, s, q, sc, r}) || overlaps(q, {in, res, w, s, sc, r}) || overlaps(sc, {in, res, w, s, r}) ||
+      overlaps(r, {in, res, w, s}) || overlaps(s, {w}) || (sum != x && overlaps(s, {in})) || (sum != residual && overlaps(s, {res})))
+    return MOE_ERR_INVALID_ARG;
   if (rows == 0) return MOE_OK;
   NormArgs a{x, residual, weight, sum, y, static_cast<uint8_t *>(codes), scales, rstd, rows, cols, eps, 1.0f / (float)cols};
   begin_launches();
@@ -532,6 +554,13 @@ extern "C" int moe_rmsnorm_backward(int64_t rows, int cols, int dtype, const voi
       !aligned4(rstd) || !aligned4(dweight) || (dweight && !aligned16(workspace)))
     return MOE_ERR_INVALID_ARG;
   if (dx == sum) return MOE_ERR_INVALID_ARG;
+  const size_t cells = (size_t)rows * cols, elt = dtype == MOE_BF16 ? 2 : 4;
+  const Extent s{sum, cells * elt}, w{weight, cols * elt}, r{rstd, rows * sizeof(float)}, g{dy, cells * elt}, ds{dsum, cells * elt},
+      out{dx, cells * elt}, dw{dweight, cols * sizeof(float)},
+      ws{dweight ? workspace : nullptr, moe_rmsnorm_backward_workspace_bytes(rows, cols)};
+  if (overlaps(out, {s, w, r, dw, ws}) || overlaps(dw, {s, w, r, g, ds, ws}) || overlaps(ws, {s, w, r, g, ds}) ||
+      (dx != dy && overlaps(out, {g})) || (dx != dsum && overlaps(out, {ds})))
+    return MOE_ERR_INVALID_ARG;
   hipStream_t st = (hipStream_t)stream;
   begin_launches();
   if (rows == 0) {
