@@ -99,10 +99,10 @@ class MoELayer:
     def norm(self, h, residual=None, codes: bool = False) -> None:
         """x (and, for forward_fp8_codes, its codes) from the output h of what comes before the layer; with a residual the new
         one is left in ``norm_sum``.  norm_backward reads that (without a residual h) again."""
-        self._normed = h if residual is None else self.norm_sum
         B.moe_rmsnorm(self.shape.T, self.shape.d, self.shape.dtype, h, residual, self.norm_weight, self.norm_eps,
                       None if residual is None else self.norm_sum, self.x, self.x_codes if codes else None,
                       self.x_scales if codes else None, self.rstd)
+        self._normed = h if residual is None else self.norm_sum
 
     def norm_backward(self, dx, dsum, dh) -> None:
         """dh from the gradient dx of the layer's input and dsum of the residual stream (or None); d_norm_weight."""

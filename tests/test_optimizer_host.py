@@ -116,3 +116,21 @@ def test_refused_step_leaves_the_rate(packs, monkeypatch):
             opt.step(lr=-1.0)
     opt.step()
     assert opt.steps == 1 and abs(opt.config.now.lr - 1e-3) < 1e-9
+
+
+def test_refused_norm_leaves_what_its_gradient_reads(monkeypatch):
+    lay, _ = layer_and_weights()
+    lay.enable_norm(torch.ones(lay.shape.d, dtype=torch.bfloat16))
+    seen = []
+    monkeypatch.setattr(B, "moe_rmsnorm", lambda *a, **k: None)
+    monkeypatch.setattr(B, "moe_rmsnorm_backward", lambda rows, cols, dtype, s, *a, **k: seen.append(s))
+    h = torch.zeros_like(lay.x)
+    lay.norm(h)
+
+    def refuse(*a, **k):
+        raise B.MoeError(B.MOE_ERR_INVALID_ARG, "moe_rmsnorm")
+    monkeypatch.setattr(B, "moe_rmsnorm", refuse)
+    with pytest.raises(B.MoeError):
+        lay.norm(h, residual=lay.x)
+    lay.norm_backward(lay.x, None, lay.x)
+    assert seen[0] is h
