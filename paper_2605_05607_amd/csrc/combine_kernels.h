@@ -94,8 +94,10 @@ __global__ __launch_bounds__(kCombineWaves * 64) void combine_kernel(const float
 
 // ------------------------------------------------------------------------------------------------
 // Dispatch as a materialised copy (phase-split entry point): one workgroup per local dedup entry reads the
-// token row once and writes it to the layout row of every slot in the entry's mask, with the non-temporal hint (nothing of
-// the call reads it again; 5003 tokens of 2880: 15 to 11 us, 8192 of 4096: 25 to 24).
+// token row once and writes it to the layout row of every slot in the entry's mask.  Without the non-temporal hint: with it the
+// copy alone is faster (one of 8 ranks, 4096 tokens of 7168 19.0 us against 21.5), and with the product that reads the rows behind it
+// slower by up to 2 % (that copy and 2 x 2048 columns 227.2 against 226.1, 8192 tokens of 4096 and 2 x 1536 columns 199.5 against
+// 195.5; 5003 of 2880 and 2 x 2880 163.9 against 162.0).
 // ------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void dispatch_gather_kernel(const uint4 *__restrict__ x,
                                                               const int32_t *__restrict__ rank_offsets,
@@ -120,8 +122,7 @@ __global__ __launch_bounds__(256) void dispatch_gather_kernel(const uint4 *__res
       m &= m - 1;
       if (j >= k) break;
       const int row = inv_perm[(size_t)t * k + j] - base;
-      if (row >= 0 && row < P_cap)
-        __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4 *>(xs) + (size_t)row * row_chunks + c);
+      if (row >= 0 && row < P_cap) xs[(size_t)row * row_chunks + c] = v;
     }
   }
 }
