@@ -447,7 +447,8 @@ MOE355_API int moe_route_backward(const moe_shape *shape, const int32_t *topk_id
  * At least one of y and codes is given; `sum` only with a residual, and it may be x or residual itself; else no array that is
  * written may overlap another one.  eps > 0.  Pointers 16-byte aligned (codes 8, scales and rstd 4).  A row with a NaN, an
  * infinity or values whose squares leave the range of fp32 (magnitudes of about 1e19) has no defined y, and a scale that is not
- * finite where y is not.
+ * finite where y is not.  Sums in fp32 in an order that depends on rows and cols: same inputs, same bits, but a row may get other last
+ * bits (and a code next to a border the other one) in a batch of another size.
  *
  * moe_rmsnorm_backward: with a = dy weight,
  *   dx = rstd (a - s rstd^2 mean(a s)) + dsum,   dweight[c] = sum over the rows of dy s rstd.
@@ -501,6 +502,8 @@ MOE355_API int moe_dispatch_gather_backward(const moe_shape *shape, const void *
  *     z ^ z >> 16 (mod 2^32), element i of tensor k of the list has h = mix(low word of i ^ mix(high word of i + mix(seed +
  *     mix(t + mix(k + 0x9E3779B9))))), m its low and sqrt(v) its high half.  A positive sqrt(v) never gets code 0.
  *     A block that holds a value that is not finite gets the scale NaN.
+ * A v below the range of fp32 is 0 (of gradients below about 3e-23 / sqrt(1 - beta2); 8 bits: a held sqrt(v) below 2^-75): where m
+ * is not 0 too, eps alone divides it.
  * The step's own numbers, moe_adamw_device, come from config->now, or, where `device` is not NULL, from that device memory when the
  * kernels run (for captured steps: write it between replays; lr, step and skipped are then not checked).  A grad_scale that is not
  * finite leaves every array as it was (a step whose gradients have overflowed is skipped without a word from the host).  step counts

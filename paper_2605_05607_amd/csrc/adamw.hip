@@ -123,9 +123,10 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
-// Parameters, states and gradients pass with the non-temporal hint, for reads and writes: a step touches each once, and all of them
-// are more than the caches hold (25 M values with 32-bit states 132 -> 114 us, 302 M with 8-bit ones 891 -> 851).  The bf16
-// copies, which the next kernels read, are written as usual.
+// Parameters, states and gradients pass with the non-temporal hint, for reads and writes: a step touches each once, and between two
+// steps lies a whole pass over the model (25 M values with 32-bit states 132 -> 114 us, 302 M with 8-bit ones 891 -> 851; lists that
+// the caches hold have the hint too, without a measurement of their own).  The bf16 copies, which the next kernels read, are written as
+// usual.
 template <typename V>
 __device__ __forceinline__ V get(const V *p) { return __builtin_nontemporal_load(p); }
 template <typename V>
@@ -295,7 +296,8 @@ struct AdamQuad {
 // PER blocks of 256 values for a wave, one behind the other; all are requested before the first is worked on.  32-bit
 // states: two.  8-bit states, whose blocks take 350 vector instructions each: four where a launch has the values to fill the chip
 // with that, else one (bf16 gradients and copies, 2^18 / 2^20 / 2^22 / 2^23 / 2^24 / 2^25 values: one block 3.5, 5.8, 15.8, 26.7, 51.5
-// and 97.9 us, four 5.8, 7.8, 16.8, 27.2, 48.3 and 89.1).
+// and 97.9 us, four 5.8, 7.8, 16.8, 27.2, 48.3 and 89.1; they cross between 2^23 and 2^24, and lists between the line and there lose 2 %
+// at 2^23).
 constexpr int kAdamFew = 1 << 22;
 constexpr int64_t adam_chunk_values(int per) { return (int64_t)per * kAdamThreads * 4; }
 template <bool EIGHT, bool BF16, int PER>

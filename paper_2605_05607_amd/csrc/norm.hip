@@ -1,11 +1,12 @@
 // Root-mean-square norm in front of the layer, with the addition of the residual, the E4M3 codes of the result for the FP8
-// form of the expert GEMMs (reading: one scale per row, largest magnitude / 448) and the gradients.
+// form of the expert GEMMs (one scale per row, largest magnitude / 448; code = cvt(y / scale)) and the gradients.
 //
 //   forward   s = round(x + residual),  rstd = (mean(s^2) + eps)^-1/2,  y = s rstd w
 //   backward  a = dy w,  dx = rstd (a - s rstd^2 mean(a s)) + dsum,  dw = sum over the rows of dy s rstd
 //
 // Bound by HBM: a handful of fp32 operations per element read.  A row stays in the registers of its threads from its one read
-// to its writes; statistics and all sums are fp32, and what is stored in the element type is rounded once.
+// to its writes, but for two forms of the gradients that read it twice, from the caches: rows of more than 32 KiB, and the weight's
+// gradient of few rows.  Statistics and all sums are fp32, and what is stored in the element type is rounded once.
 #include <algorithm>
 #include <initializer_list>
 
@@ -72,7 +73,7 @@ struct NormArgs {
 };
 
 // WAVES waves (1: four rows a workgroup, each its own wave; else one row a workgroup) with CHUNKS sixteen-byte pieces a thread.
-// 4096 x 7168 in bf16 with residual, sum, y and codes: 46 us, 5.7 TB/s of what it has to move; one row 3.6 us.
+// 4096 x 7168 in bf16 with residual, sum, y and codes: 49 us, 5.4 TB/s of what it has to move; one row 3.2 us.
 template <typename T, int WAVES, int CHUNKS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void rmsnorm_kernel(const NormArgs a) {
   constexpr int N = Piece<T>::N, STRIDE = WAVES * 64 * N;

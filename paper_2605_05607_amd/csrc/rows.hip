@@ -22,8 +22,9 @@ struct RowsArgs {
 };
 
 constexpr int kRowsWaves = 4;  // tokens per workgroup: one per wave
-// Above, a wave takes four pieces of 512 columns (fp32: two; 8192 x 4096 62.6 us against 68.5) and y leaves with the non-temporal hint; up to here one piece, so that there are
-// waves enough, and plain stores.  Microseconds of the two forms (few / many), bf16:
+// Above, a wave takes four pieces of 512 columns (fp32: two; 8192 x 4096 62.6 us against 68.5) and bf16 rows of y leave with the
+// non-temporal hint; up to here one piece, so that there are waves enough, and plain stores.  Microseconds of the two forms (few /
+// many), bf16:
 //   tokens                       64           512          1024         1536          3000
 //   7168, 1 of 8 ranks, k = 8    2.8 / 3.5    5.1 / 5.2    6.7 / 7.0    11.3 / 9.1    21.3 / 18.3
 //   2880, 1 of 4, k = 4          2.7 / 3.4    3.3 / 3.7    4.7 / 4.7     5.7 / 5.4     8.0 / 7.6
@@ -51,9 +52,10 @@ __device__ __forceinline__ Slot slot_of_lane(const RowsArgs &a, int t, int lane)
 }
 
 // One wave per token and part of its columns (blockIdx.y of gridDim.y parts, taken in turn): PIECES pieces of 512 columns at a
-// time, and the loads of two slots in flight together.  STREAM: y leaves with the non-temporal hint.  LAST: the rows come with it too
-// (the sorting copy's gradient, whose rows nothing reads again: 5003 tokens of 2880 with everything 54.5 -> 50.8 us, 8192 of 4096 114
-// -> 112; the experts' rows are read again by their gradient).
+// time, and the loads of two slots in flight together.  STREAM: y leaves with the non-temporal hint, in bf16 (alone, 8192 tokens of 4096
+// 24.6 us against 30.0; the norm that reads y right behind it gives more than that back: both together 78.6 against 78.4, and 4096
+// tokens of 7168 71.8 against 65.7).  LAST: the rows come with it too (the sorting copy's gradient, whose rows nothing reads again: 5003
+// tokens of 2880 with everything 54.5 -> 50.8 us, 8192 of 4096 114 -> 112; the experts' rows are read again by their gradient).
 template <typename T, int PIECES, bool STREAM, bool LAST>
 __global__ __launch_bounds__(kRowsWaves * 64) void combine_rows_kernel(const RowsArgs a) {
   const int lane = threadIdx.x & 63;
@@ -108,7 +110,9 @@ __global__ __launch_bounds__(kRowsWaves * 64) void combine_rows_kernel(const Row
 }
 
 // One workgroup per token, two slots at a time (k = 8, all local: 128 tokens of 4096 10.0 us with one, 8.3; 4096 of 7168 211 and 208, 4.8
-// TB/s).  A slot's dot product: per thread over its columns, then over the waves in LDS.
+// TB/s).  A slot's dot product: per thread over its columns, then over the waves in LDS.  d_rows leave with the non-temporal hint in bf16
+// (a training step's four calls around the experts, 8192 tokens of 4096, 112.5 us against 115.3, 5003 of 2880 49.9 against 54.6, where
+// nothing reads the rows; with a product of 256 columns right behind, 4096 tokens of 7168, 104.7 against 101.0).
 constexpr int kBackThreads = 256;
 template <typename T>
 __global__ __launch_bounds__(kBackThreads) void combine_rows_backward_kernel(const RowsArgs a) {
