@@ -496,9 +496,10 @@ MOE355_API int moe_dispatch_gather_backward(const moe_shape *shape, const void *
  * grad_dtype, all 16-byte aligned; n = 0 is an empty tensor.  No array that is written may overlap another one of the call.
  *   state_bits 32: m, v fp32 [n], 16-byte aligned; the scales are not read.
  *   state_bits 8:  m, v uint8 [n], 16-byte aligned, m_scale, v_scale fp32 [ceil(n / MOE_ADAMW_BLOCK)]: E4M3 codes of m / scale and
- *     of sqrt(v) / scale, one scale per MOE_ADAMW_BLOCK values = largest magnitude / 448 (1 for a block of zeros, and a block of m
- *     below 2^-100 counts as one; a fresh state is codes 0).  The step is taken with the new m and v before they are rounded.  A
- *     code is rounded up with the probability of the part that is cut off, from 16 bits of a hash: with mix(z): z = (z ^ z >> 16) * 0x6A09E667, z = (z ^ z >> 15) * 0xBB67AE85,
+ *     of sqrt(v) / scale, one scale per MOE_ADAMW_BLOCK values = largest magnitude times 1/448, both and the product in fp32 (1 for a
+ *     block of zeros, and a block of m below 2^-100 counts as one; a fresh state is codes 0); the quotient is fp32's, correctly
+ *     rounded.  The step is taken with the new m and v before they are rounded.  A code is rounded up with the probability of the
+ *     part that is cut off, from 16 bits of a hash: with mix(z): z = (z ^ z >> 16) * 0x6A09E667, z = (z ^ z >> 15) * 0xBB67AE85,
  *     z ^ z >> 16 (mod 2^32), element i of tensor k of the list has h = mix(low word of i ^ mix(high word of i + mix(seed +
  *     mix(t + mix(k + 0x9E3779B9))))), m its low and sqrt(v) its high half.  A positive sqrt(v) never gets code 0.
  *     A block that holds a value that is not finite gets the scale NaN.

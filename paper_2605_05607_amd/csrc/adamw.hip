@@ -3,7 +3,7 @@
 //   g = grad_scale grad,  m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2
 //   p = p (1 - lr decay) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
-// States in 8 bits: blocks of 256 values, each E4M3 codes of value / scale with scale = largest magnitude / 448 (1 for an
+// States in 8 bits: blocks of 256 values, each E4M3 codes of value / scale with scale = largest magnitude times 1/448 (1 for an
 // all-zero block).  The second state is held as sqrt(v), whose range is half of v's in octaves, and the step uses the new
 // states before they are rounded.  Codes are rounded up with the probability of what is cut off (16 random bits): a moving
 // average changes by less than half a code from step to step (0.1 % against 6 %), so rounding to nearest would stop it.  A
@@ -136,12 +136,13 @@ struct BlockScale {
   float scale, inv;
 };
 // The scale of the 256 values of a wave, from the largest bit pattern of their magnitudes (a NaN or an infinity gives a scale
-// of NaN, so that the block shows it): largest / 448, correctly rounded.  Below 2^-100 a block counts as zero: the reciprocal of its
-// scale is no normal number.  (Square roots of numbers in fp32 are 2^-75 and more, or 0.)
+// of NaN, so that the block shows it): one product with fp32's 1/448, which is part of the states' definition (a division gives
+// another last bit in half of the blocks, and with it other codes).  Below 2^-100 a block counts as zero: the reciprocal of its scale is
+// no normal number.  (Square roots of numbers in fp32 are 2^-75 and more, or 0.)
 __device__ __forceinline__ BlockScale block_scale(uint32_t top) {
   top = wave_max(top);
   const bool finite = top < 0x7F800000u, some = top >= 0x0D800000u;
-  const float scale = some ? quotient(__uint_as_float(top), 448.0f, 1.0f / 448.0f) : 1.0f;
+  const float scale = some ? __uint_as_float(top) * (1.0f / 448.0f) : 1.0f;
   const float r = __builtin_amdgcn_rcpf(scale);
   return {finite ? scale : __builtin_nanf(""), finite && some ? fmaf(fmaf(-scale, r, 1.0f), r, r) : 0.0f};
 }

@@ -1,5 +1,5 @@
 """8-bit states of AdamW bit for bit: the formulas evaluated in fp32, one rounding an operation, on the host.  Scales are largest
-magnitude / 448, a division; codes take the hash's bits.  Nothing is left to a tolerance."""
+magnitude times fp32's 1/448; codes take the hash's bits.  Nothing is left to a tolerance."""
 import numpy as np
 import pytest
 import torch
@@ -32,7 +32,7 @@ def decode(codes, scale):
 def encode(v, bits16, least):
     blocks = np.pad(np.abs(v), (0, -len(v) % BLOCK)).reshape(-1, BLOCK)
     top = blocks.max(1)
-    scale = np.where(top > 0, top / F(448), F(1)).astype(F)
+    scale = np.where(top > 0, top * (F(1) / F(448)), F(1)).astype(F)
     q = np.abs(v) / np.repeat(scale, BLOCK)[: len(v)]
     bits = np.minimum(q * F(2.0 ** -120), F(448 * 2.0 ** -120)).view(np.uint32)
     code = (bits + (bits16.astype(np.uint32) << np.uint32(4))) >> np.uint32(20)
