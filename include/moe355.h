@@ -476,7 +476,8 @@ MOE355_API int moe_rmsnorm_backward(int64_t rows, int cols, int dtype, const voi
  *
  * moe_combine_weighted: y[t] = sum over the local slots j of topk_w[t,j] rows[row of (t,j)], zeros where there is none.
  * moe_combine_weighted_backward: d_rows[row of (t,j)] = topk_w[t,j] dy[t], d_topk_w[t,j] = <rows[row of (t,j)], dy[t]> in fp32
- *   (0 for a slot whose expert is not local; the array is written in full).  d_rows may be rows itself.
+ *   (0 for a slot whose expert is not local; the array is written in full).  d_rows may be rows itself; else nothing that one of
+ *   the three writes may overlap another array.
  * moe_dispatch_gather_backward: dx[t] = sum over the local slots j of d_xs[row of (t,j)], zeros where there is none.
  */
 MOE355_API int moe_combine_weighted(const moe_shape *shape, const void *rows, const int32_t *topk_idx, const float *topk_w,
