@@ -277,6 +277,13 @@ class AdamW:
         words = self._device.tolist()
         return words[2] - words[4]
 
+    @steps.setter
+    def steps(self, taken: int) -> None:
+        self._steps = taken
+        if self.scalars is not None:
+            self._count.fill_(taken)
+            self._skipped.zero_()
+
     def step(self, lr=None, grad_scale=1.0) -> None:
         """One step with the gradients as they are.  lr: a new rate from now on.  grad_scale: multiplies the gradients; one that is
         not finite skips the step, which then does not count in the averages' corrections.  With device scalars both are set there."""

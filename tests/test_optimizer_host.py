@@ -134,3 +134,12 @@ def test_refused_norm_leaves_what_its_gradient_reads(monkeypatch):
         lay.norm(h, residual=lay.x)
     lay.norm_backward(lay.x, None, lay.x)
     assert seen[0] is h
+
+
+def test_steps_can_be_set(packs):
+    for device in (False, True):
+        opt = L.AdamW([torch.zeros(10)], [torch.zeros(10)], 1e-3, device_scalars=device)
+        opt.step()
+        opt.steps = 41
+        opt.step()
+        assert opt.steps == 42
